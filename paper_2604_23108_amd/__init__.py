@@ -1,7 +1,8 @@
 """MI355X (gfx950) implementation of one MoHGE layer (forward, auxiliary losses, backward)
 behind a C ABI.
 
-`binding` marshals torch tensors into the calls of `include/mohge.h`; every step
+`binding` marshals torch tensors into the calls of `include/mohge.h`, `block_binding` into those of
+`include/mohge_block.h` (what stands around the layer in a decoder block); every step
 of the layer runs in the HIP kernels of `csrc/`.  There is no CPU or PyTorch fallback:
 if `libmohge.so` has not been built, loading fails.
 """
@@ -15,4 +16,8 @@ from .binding import (  # noqa: F401
     mohge_fused_status, mohge_expert_ffn_w4, mohge_mxfp4_decode, mohge_decode_layer,
     mohge_decode_layer_ctl_bytes, CALL_DECODE_LAYER,
 )
-from .weights import quantize_rows_e4m3, quantize_mxfp4  # noqa: F401
+from .block_binding import (  # noqa: F401
+    E4M3, NormConfig, CacheConfig, ProjConfig, mohge_rmsnorm, mohge_rmsnorm_bwd, mohge_norm_workspace_size, mohge_cache_append,
+    mohge_cache_attention, mohge_cache_workspace_size, mohge_proj_w4, ResidualNorm, KVCache, ProjW4,
+)
+from .weights import quantize_rows_e4m3, quantize_mxfp4, quantize_w4  # noqa: F401

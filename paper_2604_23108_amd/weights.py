@@ -43,3 +43,20 @@ def quantize_mxfp4(w: torch.Tensor):
     return packed.contiguous(), scales.contiguous()
 
 
+def quantize_w4(w: torch.Tensor, group: int = 128, zeros: bool = False):
+    """4-bit quantisation of a weight matrix [rows, cols] for mohge_proj_w4, cols a multiple of `group`: every `group` elements of a row
+    share a bf16 scale s and a zero point z, w = s * (code - z), codes 0..15.  Without `zeros` z is 8 and s = max|group| / 7;
+    with it s = (max - min) / 15 and z the code nearest to 0 (0 lies within the range: max and min are taken with it).  s is 1 for a
+    group of zeros.  Codes are rounded to nearest even with the bf16 scale and clamped.  Returns (packed uint8 [rows, cols/2],
+    two codes per byte, even element in the low four bits; scales bf16 [rows, cols/group]; zero points uint8 of that shape, or None)."""
+    rows, K = w.shape
+    if group not in (32, 64, 128) or K % group:
+        raise ValueError(f"quantize_w4: last dimension {K} is not a multiple of a group of 32, 64 or 128 (group = {group})")
+    blk = w.float().reshape(rows, K // group, group)
+    hi, lo = blk.amax(2).clamp(min=0), blk.amin(2).clamp(max=0)
+    s = (hi - lo) / 15.0 if zeros else torch.maximum(hi, -lo) / 7.0
+    s = torch.where(s > 0, s, torch.ones_like(s)).bfloat16()
+    z = torch.round(-lo / s.float()).clamp(0, 15) if zeros else torch.full_like(hi, 8.0)
+    code = (torch.round(blk / s.float().unsqueeze(2)) + z.unsqueeze(2)).clamp(0, 15).to(torch.uint8).reshape(rows, K // 2, 2)
+    packed = code[..., 0] | (code[..., 1] << 4)
+    return packed.contiguous(), s.contiguous(), z.to(torch.uint8).contiguous() if zeros else None
