@@ -1,18 +1,21 @@
-"""ctypes binding of the operators around the layer (`include/mohge_block.h`, in libmohge.so): argument
-marshalling only, with the names and argument order of the header, plus objects that hold the buffers of one use
-(`ResidualNorm`, `KVCache`, `ProjW4`).
+"""Binding of the operators around the layer (`include/mohge_block.h`, in libmohge.so): argument marshalling only, with
+the names and argument order of the header, plus objects that hold the buffers of one use (`ResidualNorm`, `KVCache`,
+`ProjW4`).
 
 Tensors must live on the GPU and be contiguous (the rows of q, k and v may be further apart); the current torch
-stream is passed as the HIP stream.
+stream is passed as the HIP stream.  The calls of a step go through the extension module `_block_native`
+(`csrc/block_py.cpp`), the rest through ctypes.
 """
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
+import os
 from typing import Optional, Sequence
 
 import torch
 
-from .binding import BF16, F32, MohgeError, _addr, _check, _raw_stream, _size, lib
+from .binding import BF16, F32, MohgeError, lib
 
 E4M3 = 2
 
@@ -37,6 +40,27 @@ def _call(name):
         f.argtypes = [_KINDS[k] for k in _ARGS[name]]
         _calls[name] = f
     return f
+
+
+class _Native:
+    """The extension module, loaded and given the library's entry points at the first call."""
+
+    def __getattr__(self, name):
+        path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_block_native.so")
+        if not os.path.exists(path):
+            raise MohgeError(f"{path} is missing: build it with `python -m paper_2604_23108_amd.build` (there is no fallback path)")
+        spec = importlib.util.spec_from_file_location("_block_native", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        entries = ("mohge_rmsnorm", "mohge_rmsnorm_bwd", "mohge_cache_append", "mohge_cache_attention", "mohge_proj_w4",
+                   "mohge_last_error")
+        module.bind(MohgeError, *[C.cast(getattr(lib(), e), C.c_void_p).value for e in entries])
+        for n in ("rmsnorm", "rmsnorm_bwd", "cache_append", "cache_attention", "proj_w4"):
+            setattr(self, n, getattr(module, n))
+        return self.__dict__[name]
+
+
+_native = _Native()
 
 
 class _CNorm(C.Structure):
@@ -93,35 +117,8 @@ class ProjConfig:
         self.ref = C.addressof(self._c)
 
 
-def _expect(name: str, t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype):
-    """The address of a tensor that has to have this shape and type (None stays None: the library says what it needs)."""
-    if t is None:
-        return None
-    if t.shape != shape or t.dtype != dtype:
-        raise MohgeError(f"{name}: {tuple(t.shape)} {t.dtype} given, {shape} {dtype} needed")
-    return _addr(t)
-
-
-def _rows(name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype):
-    """Address and row stride of [rows, heads, size] whose rows are contiguous but may be further apart."""
-    if t.shape != shape or t.dtype != dtype:
-        raise MohgeError(f"{name}: {tuple(t.shape)} {t.dtype} given, {shape} {dtype} needed")
-    if not t.is_cuda:
-        raise MohgeError("tensors handed to the library must be on the GPU")
-    width = shape[1] * shape[2]
-    step, head, one = t.stride()
-    if one != 1 or (head != shape[2] and shape[1] > 1):
-        raise MohgeError(f"{name}: the heads of a row must be contiguous")
-    return t.data_ptr(), step if shape[0] > 1 else width
-
-
 def mohge_rmsnorm(cfg: NormConfig, x, residual, weight, sum_out, y, y_scale=None, rstd=None):
-    t, shape = _TORCH[cfg.dtype], (cfg.T, cfg.d)
-    _check(_call("mohge_rmsnorm")(cfg.ref, _expect("x", x, shape, t), _expect("residual", residual, shape, t),
-                                  _expect("weight", weight, (cfg.d,), torch.float32), _expect("sum_out", sum_out, shape, t),
-                                  _expect("y", y, shape, _TORCH[cfg.y_dtype]),
-                                  _expect("y_scale", y_scale, (cfg.T,), torch.float32),
-                                  _expect("rstd", rstd, (cfg.T,), torch.float32), _raw_stream()), "mohge_rmsnorm")
+    _native.rmsnorm(cfg.ref, x, residual, weight, sum_out, y, y_scale, rstd)
 
 
 def mohge_norm_workspace_size(cfg: NormConfig) -> int:
@@ -129,31 +126,12 @@ def mohge_norm_workspace_size(cfg: NormConfig) -> int:
 
 
 def mohge_rmsnorm_bwd(cfg: NormConfig, dy, h, weight, rstd, dsum, dx, dweight, workspace):
-    t, shape = _TORCH[cfg.dtype], (cfg.T, cfg.d)
-    _check(_call("mohge_rmsnorm_bwd")(cfg.ref, _expect("dy", dy, shape, t), _expect("h", h, shape, t),
-                                      _expect("weight", weight, (cfg.d,), torch.float32),
-                                      _expect("rstd", rstd, (cfg.T,), torch.float32), _expect("dsum", dsum, shape, t),
-                                      _expect("dx", dx, shape, t), _expect("dweight", dweight, (cfg.d,), torch.float32),
-                                      _addr(workspace), _size(workspace), _raw_stream()), "mohge_rmsnorm_bwd")
-
-
-def _cache_args(cfg: CacheConfig, block_table, seq_lens, k_pages, v_pages, k_scale, v_scale):
-    pages, t = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_size), _TORCH[cfg.cache_dtype]
-    return (_expect("block_table", block_table, (cfg.n_seqs, cfg.max_pages), torch.int32),
-            _expect("seq_lens", seq_lens, (cfg.n_seqs,), torch.int32), _expect("k_pages", k_pages, pages, t),
-            _expect("v_pages", v_pages, pages, t), _expect("k_scale", k_scale, pages[:3], torch.float32),
-            _expect("v_scale", v_scale, pages[:3], torch.float32))
+    _native.rmsnorm_bwd(cfg.ref, dy, h, weight, rstd, dsum, dx, dweight, workspace)
 
 
 def mohge_cache_append(cfg: CacheConfig, k, v, tok_offsets, block_table, seq_lens, k_pages, v_pages, k_scale=None,
                        v_scale=None):
-    n, t = k.shape[0], _TORCH[cfg.dtype]
-    kp, ks = _rows("k", k, (n, cfg.n_kv_heads, cfg.head_size), t)
-    vp, vs = _rows("v", v, (n, cfg.n_kv_heads, cfg.head_size), t)
-    _check(_call("mohge_cache_append")(cfg.ref, n, kp, ks, vp, vs,
-                                       _expect("tok_offsets", tok_offsets, (cfg.n_seqs + 1,), torch.int32),
-                                       *_cache_args(cfg, block_table, seq_lens, k_pages, v_pages, k_scale, v_scale),
-                                       _raw_stream()), "mohge_cache_append")
+    _native.cache_append(cfg.ref, k, v, tok_offsets, block_table, seq_lens, k_pages, v_pages, k_scale, v_scale)
 
 
 def mohge_cache_workspace_size(cfg: CacheConfig) -> int:
@@ -162,23 +140,11 @@ def mohge_cache_workspace_size(cfg: CacheConfig) -> int:
 
 def mohge_cache_attention(cfg: CacheConfig, q, block_table, seq_lens, k_pages, v_pages, k_scale, v_scale, scale: float,
                           out, lse, workspace):
-    t = _TORCH[cfg.dtype]
-    qp, qs = _rows("q", q, (cfg.n_seqs, cfg.n_heads, cfg.head_size), t)
-    _check(_call("mohge_cache_attention")(cfg.ref, qp, qs, *_cache_args(cfg, block_table, seq_lens, k_pages, v_pages,
-                                                                       k_scale, v_scale), scale,
-                                          _expect("out", out, (cfg.n_seqs, cfg.n_heads, cfg.head_size), t),
-                                          _expect("lse", lse, (cfg.n_seqs, cfg.n_heads), torch.float32),
-                                          _addr(workspace), _size(workspace), _raw_stream()), "mohge_cache_attention")
+    _native.cache_attention(cfg.ref, q, block_table, seq_lens, k_pages, v_pages, k_scale, v_scale, scale, out, lse, workspace)
 
 
 def mohge_proj_w4(cfg: ProjConfig, x, x_scale, codes, scales, zeros, y):
-    per = (cfg.n_out, cfg.n_in // cfg.group if cfg.group else 0)
-    _check(_call("mohge_proj_w4")(cfg.ref, _expect("x", x, (cfg.T, cfg.n_in), _TORCH[cfg.x_dtype]),
-                                  _expect("x_scale", x_scale, (cfg.T,), torch.float32),
-                                  _expect("codes", codes, (cfg.n_out, cfg.n_in // 2), torch.uint8),
-                                  _expect("scales", scales, per, torch.bfloat16),
-                                  _expect("zeros", zeros, per, torch.uint8),
-                                  _expect("y", y, (cfg.T, cfg.n_out), _TORCH[cfg.y_dtype]), _raw_stream()), "mohge_proj_w4")
+    _native.proj_w4(cfg.ref, x, x_scale, codes, scales, zeros, y)
 
 
 class ResidualNorm:
