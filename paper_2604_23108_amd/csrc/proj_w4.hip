@@ -13,6 +13,8 @@
 //   sums of x           a product with ones gives sum_{k in g} x_tk in the lanes that need it.
 //   groups              one product reduces 8 codes of each of four lanes; with groups of 128 those are in one group as
 //                       loaded, for 64 and 32 the lanes exchange words first (v_permlane32_swap, v_permlane16_swap).
+#include <type_traits>
+
 #include "block.h"
 
 namespace mohge {
@@ -59,6 +61,8 @@ __device__ __forceinline__ int index_of(int w, int q) {
   else return 32 * w + 8 * q;
 }
 
+constexpr int proj_batch(int group, int nt) { return (group == 32 ? 2 : 4) / nt; }      // (what the registers hold)
+
 struct ProjArgs {
   const void* x;
   const float* x_scale;
@@ -67,82 +71,106 @@ struct ProjArgs {
   const unsigned char* zeros;
   void* y;
   int T, n_in, n_out, f32;
-  int units;          // units staged at a time, a power of two; a unit is 128 indices (64 bytes) of a weight row
-  int shift;          // log2 of the pieces of 8 indices in a staged row, units * 16
 };
 
-// 8 elements of x: requested, and later put to LDS as bf16 in the order 0 4 1 5 2 6 3 7
-template <bool E4M3>
-struct Eight {
-  uint32_t d[E4M3 ? 2 : 4];
-  __device__ __forceinline__ void load(const void* x, long long at, bool in) {
+// A unit is 128 indices (64 bytes) of a weight row; U units are requested, staged and multiplied together.
+
+// U units of the rows of x on their way to LDS: pieces of 8 elements, requested by N threads, P each, and later put there as bf16 in
+// the order 0 4 1 5 2 6 3 7.  What depends on the thread alone is worked out once.
+template <bool E4M3, int U, int N, int P>
+struct Staged {
+  static constexpr int kPitch = U * 256 + 16, kUnit = E4M3 ? 128 : 256;          // bytes of a unit of a row in LDS with 16 to spare, in x
+  typedef typename std::conditional<E4M3, uint2, uint4>::type Piece8;
+  Piece8 d[P];
+  uint32_t from[P];          // byte in x of the piece of unit 0
+  int to[P];                 // byte in LDS, or -1
+  __device__ __forceinline__ void init(const ProjArgs& a, const int thread) {
 #pragma unroll
-    for (int i = 0; i < (E4M3 ? 2 : 4); ++i) d[i] = 0u;
-    if (!in) return;
-    if constexpr (E4M3) {
-      const uint2 c = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(x) + at);
-      d[0] = c.x; d[1] = c.y;
-    } else {
-      const uint4 c = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at);
-      d[0] = c.x; d[1] = c.y; d[2] = c.z; d[3] = c.w;
+    for (int j = 0; j < P; ++j) {
+      const int i = thread + N * j, t = i / (U * 16), p = i % (U * 16);
+      to[j] = t < a.T ? t * kPitch + 16 * p : -1;
+      from[j] = (uint32_t)(min(t, a.T - 1) * a.n_in + 8 * p) * (E4M3 ? 1u : 2u);
     }
   }
-  __device__ __forceinline__ void store(unsigned char* to) const {
-    uint32_t w[4];
-    if constexpr (E4M3) {
+  // units from u0 on, all within the rows
+  __device__ __forceinline__ void request(const ProjArgs& a, const int u0) {
+    const unsigned char* base = static_cast<const unsigned char*>(a.x) + u0 * kUnit;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {                       // exact: the upper halves of the fp32 patterns
-        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[j], false);
-        const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[j], true);
-        w[2 * j] = __builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), 0x07060302u);
-        w[2 * j + 1] = __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), 0x07060302u);
+    for (int j = 0; j < P; ++j) d[j] = *reinterpret_cast<const Piece8*>(base + from[j]);
+  }
+  // the same where the rows end within the units: zero past them
+  __device__ __forceinline__ void request_last(const ProjArgs& a, const int u0) {
+    const unsigned char* base = static_cast<const unsigned char*>(a.x) + u0 * kUnit;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      d[j] = Piece8();
+      const int p = ((to[j] >= 0 ? to[j] : 0) % kPitch) / 16;
+      if (to[j] >= 0 && u0 * 128 + 8 * p < a.n_in) d[j] = *reinterpret_cast<const Piece8*>(base + from[j]);
+    }
+  }
+  __device__ __forceinline__ void put(unsigned char* lds) const {
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      uint4 o;
+      if constexpr (E4M3) {                                // exact: the upper halves of the fp32 patterns
+        const auto u0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[j].x, false), u1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[j].x, true);
+        const auto v0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[j].y, false), v1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d[j].y, true);
+        o = make_uint4(__builtin_amdgcn_perm(__float_as_uint(v0[0]), __float_as_uint(u0[0]), 0x07060302u),
+                       __builtin_amdgcn_perm(__float_as_uint(v0[1]), __float_as_uint(u0[1]), 0x07060302u),
+                       __builtin_amdgcn_perm(__float_as_uint(v1[0]), __float_as_uint(u1[0]), 0x07060302u),
+                       __builtin_amdgcn_perm(__float_as_uint(v1[1]), __float_as_uint(u1[1]), 0x07060302u));
+      } else {
+        o = make_uint4(__builtin_amdgcn_perm(d[j].z, d[j].x, 0x05040100u), __builtin_amdgcn_perm(d[j].z, d[j].x, 0x07060302u),
+                       __builtin_amdgcn_perm(d[j].w, d[j].y, 0x05040100u), __builtin_amdgcn_perm(d[j].w, d[j].y, 0x07060302u));
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = d[j];
+      if (to[j] >= 0) *reinterpret_cast<uint4*>(lds + to[j]) = o;
     }
-    *reinterpret_cast<uint4*>(to) =
-        make_uint4(__builtin_amdgcn_perm(w[2], w[0], 0x05040100u), __builtin_amdgcn_perm(w[2], w[0], 0x07060302u),
-                   __builtin_amdgcn_perm(w[3], w[1], 0x05040100u), __builtin_amdgcn_perm(w[3], w[1], 0x07060302u));
   }
 };
 
-// RT blocks of 16 weight rows: the codes of U units, requested together, with their scales and zero points
-template <int GROUP, int RT, int U>
+// RT blocks of 16 weight rows: the codes of U units with their scales and zero points
+template <int GROUP, int RT, int U, bool Z>
 struct Batch {
   static constexpr int kPer = 128 / GROUP;             // groups in a unit
   uint4 w[RT][U];
-  uint32_t s[RT][U * kPer / 2];                         // bf16 pairs
+  uint32_t s[RT][(U * kPer + 1) / 2];                   // bf16 pairs
   uint32_t z[RT][(U * kPer + 3) / 4];                   // up to four bytes each
 
-  // units u0 .. u0 + U - 1, those before `end`
-  __device__ __forceinline__ void load(const ProjArgs& a, const int (&row)[RT], int u0, int end, int q) {
+  // units u0 .. u0 + U - 1, all within the row.  (No condition anywhere: the same number of loads every time, so that the waits
+  // for the batch before can be counted instead of waiting for everything.)
+  __device__ __forceinline__ void load(const ProjArgs& a, const int (&row)[RT], int u0, int q) {
     const int groups = a.n_in / GROUP, g0 = u0 * kPer;
-    if (u0 + U <= end && (u0 + U) * 128 <= a.n_in) {
 #pragma unroll
-      for (int f = 0; f < RT; ++f) {
-        const unsigned char* cp = a.codes + (long long)row[f] * (a.n_in / 2) + u0 * 64 + 16 * q;
+    for (int f = 0; f < RT; ++f) {
+      const unsigned char* cp = a.codes + (long long)row[f] * (a.n_in / 2) + u0 * 64 + 16 * q;
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[f][u] = *reinterpret_cast<const uint4*>(cp + 64 * u);
-        __builtin_memcpy(s[f], a.scales + (long long)row[f] * groups + g0, sizeof(s[f]));       // (rows need not be aligned)
-        if (a.zeros) __builtin_memcpy(z[f], a.zeros + (long long)row[f] * groups + g0, U * kPer);
+      for (int u = 0; u < U; ++u) w[f][u] = *reinterpret_cast<const uint4*>(cp + 64 * u);
+      __builtin_memcpy(s[f], a.scales + (long long)row[f] * groups + g0, 2 * U * kPer);          // (rows need not be aligned)
+      if constexpr (Z) __builtin_memcpy(z[f], a.zeros + (long long)row[f] * groups + g0, U * kPer);
+    }
+  }
+  // the last units, those before `end`: codes, scales and zero points of the others are 0
+  __device__ __forceinline__ void load_last(const ProjArgs& a, const int (&row)[RT], int u0, int end, int q) {
+    const int groups = a.n_in / GROUP;
+#pragma unroll
+    for (int f = 0; f < RT; ++f) {
+      const unsigned char* cp = a.codes + (long long)row[f] * (a.n_in / 2);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = (u0 + u) * 64 + 16 * q;
+        w[f][u] = make_uint4(0u, 0u, 0u, 0u);
+        if (u0 + u < end && k < a.n_in / 2) w[f][u] = *reinterpret_cast<const uint4*>(cp + k);
       }
-    } else {
 #pragma unroll
-      for (int f = 0; f < RT; ++f) {
-        const unsigned char* cp = a.codes + (long long)row[f] * (a.n_in / 2) + u0 * 64 + 16 * q;
+      for (int i = 0; i < (U * kPer + 1) / 2; ++i) s[f][i] = 0u;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          w[f][u] = make_uint4(0u, 0u, 0u, 0u);
-          if (u0 + u < end && (u0 + u) * 128 + 32 * q < a.n_in) w[f][u] = *reinterpret_cast<const uint4*>(cp + 64 * u);
-        }
+      for (int i = 0; i < (U * kPer + 3) / 4; ++i) z[f][i] = 0u;
 #pragma unroll
-        for (int g = 0; g < U * kPer; ++g) {
-          const bool in = g0 + g < end * kPer && g0 + g < groups;
-          const uint32_t sv = in ? a.scales[(long long)row[f] * groups + g0 + g] : 0u;
-          const uint32_t zv = in && a.zeros ? a.zeros[(long long)row[f] * groups + g0 + g] : 0u;
-          s[f][g / 2] = g & 1 ? s[f][g / 2] | sv << 16 : sv;
-          z[f][g / 4] = g & 3 ? z[f][g / 4] | zv << (8 * (g & 3)) : zv;
+      for (int i = 0; i < U * kPer; ++i) {
+        const int g = u0 * kPer + i;
+        if (g < end * kPer && g < groups) {
+          s[f][i / 2] |= (uint32_t)a.scales[(long long)row[f] * groups + g] << (16 * (i & 1));
+          if constexpr (Z) z[f][i / 4] |= (uint32_t)a.zeros[(long long)row[f] * groups + g] << (8 * (i & 3));
         }
       }
     }
@@ -150,9 +178,9 @@ struct Batch {
 };
 
 // acc += unit u of the batch; x: LDS address of the unit in row 16 t + m of x
-template <int GROUP, int RT, int NT, int U>
-__device__ __forceinline__ void multiply(const Batch<GROUP, RT, U>& b, const int u, const bool zeros,
-                                         const unsigned char* const (&x)[NT], const int q, f32x4 (&acc)[RT][NT]) {
+template <int GROUP, int RT, int NT, int U, bool Z>
+__device__ __forceinline__ void multiply(const Batch<GROUP, RT, U, Z>& b, const int u, const unsigned char* const (&x)[NT], const int q,
+                                         f32x4 (&acc)[RT][NT]) {
   constexpr int kPer = 128 / GROUP, kWords = 4 / kPer;
   ProjFrag ones;
 #pragma unroll
@@ -195,7 +223,8 @@ __device__ __forceinline__ void multiply(const Batch<GROUP, RT, U>& b, const int
     for (int f = 0; f < RT; ++f) {
       const int at = u * kPer + g;
       const float s = __uint_as_float(at & 1 ? b.s[f][at / 2] & 0xffff0000u : b.s[f][at / 2] << 16);
-      const float z = zeros ? 16.f + (float)((b.z[f][at / 4] >> (8 * (at & 3))) & 255u) : 24.f;
+      float z = 24.f;
+      if constexpr (Z) z = 16.f + (float)((b.z[f][at / 4] >> (8 * (at & 3))) & 255u);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -227,109 +256,96 @@ __device__ __forceinline__ void store_rows(const ProjArgs& a, const int n0, cons
     }
 }
 
-// Few weight rows: a workgroup has 16 RT of them, its KW waves a part of the reduction each.  A wave stages its own part of
-// x without a barrier, and has NB batches of two units on the way while it multiplies.
-template <int GROUP, int NT, int RT, int KW, int NB, bool E4M3>
+// Few weight rows: a workgroup has 16 of them, its KW waves a part of the reduction each.  A wave stages its own part of x, U
+// units at a time and without a barrier.
+// P pieces of x per lane.
+template <int GROUP, int NT, int KW, int U, int P, bool Z, bool E4M3>
 __global__ void __launch_bounds__(64 * KW) proj_w4_split_kernel(const ProjArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  constexpr int U = 2;
+  constexpr int kPitch = U * 256 + 16;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, q = lane >> 4;
-  const int n0 = blockIdx.x * 16 * RT;
-  int row[RT];
-#pragma unroll
-  for (int f = 0; f < RT; ++f) row[f] = min(n0 + 16 * f + m, a.n_out - 1);
+  const int n0 = blockIdx.x * 16;
+  const int row[1] = {min(n0 + m, a.n_out - 1)};
   const int nu = (a.n_in + 127) / 128, ub = nu * w / KW, ue = nu * (w + 1) / KW;
-  const int pitch = a.units * 256 + 16, all = a.T << a.shift;
-  unsigned char* const mine = lds + w * a.T * pitch;
+  unsigned char* const mine = lds + w * a.T * kPitch;
   const unsigned char* xrow[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) xrow[t] = mine + min(16 * t + m, a.T - 1) * pitch;
-  // x of the units from uc on: kPieces per lane requested, and later put to LDS
-  constexpr int kPieces = 4 * NT;
-  Eight<E4M3> e[kPieces];
-  auto request = [&](int uc, int i0) {
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = i0 + 64 * j, t = i >> a.shift, k = uc * 128 + 8 * (i - (t << a.shift));
-      if (i0 - lane + 64 * j < all)                 // (wave-uniform: no address for nothing)
-        e[j].load(a.x, (long long)t * a.n_in + k, i < all && k < a.n_in);
-    }
-  };
-  auto put = [&](int i0) {
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = i0 + 64 * j, t = i >> a.shift;
-      if (i < all) e[j].store(mine + t * pitch + 16 * (i - (t << a.shift)));
-    }
-  };
-  // what is waited for first is requested first
-  request(ub, lane);
-  Batch<GROUP, RT, U> b[NB];
-#pragma unroll
-  for (int i = 0; i < NB; ++i) b[i].load(a, row, ub + U * i, ue, q);
-  f32x4 acc[RT][NT];
-#pragma unroll
-  for (int f = 0; f < RT; ++f)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // (units: a multiple of NB * U, or all of the wave's)
-  for (int uc = ub; uc < ue; uc += a.units) {
-    if (uc > ub) request(uc, lane);
-    put(lane);
-    for (int i0 = lane + 64 * kPieces; i0 - lane < all; i0 += 64 * kPieces) {
-      request(uc, i0);
-      put(i0);
-    }
+  for (int t = 0; t < NT; ++t) xrow[t] = mine + min(16 * t + m, a.T - 1) * kPitch;
+  Staged<E4M3, U, 64, P> x;
+  x.init(a, lane);
+  auto put = [&]() {
+    x.put(mine);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int last = min(uc + a.units, ue);
-    for (int u0 = uc; u0 < last; u0 += U * NB) {
+  };
+  f32x4 acc[1][NT];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        if (u0 + U * i < last) {                       // wave-uniform; past an odd end codes, scales and zero points are 0
+  for (int t = 0; t < NT; ++t) acc[0][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Batch<GROUP, 1, U, Z> cur, next;
+  auto compute = [&]() {
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const unsigned char* x[NT];
+    for (int u = 0; u < U; ++u) {
+      const unsigned char* at[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) x[t] = xrow[t] + (u0 - uc + U * i + u) * 256;
-            multiply<GROUP, RT, NT, U>(b[i], u, a.zeros != nullptr, x, q, acc);
-          }
-          if (u0 + U * (NB + i) < ue) b[i].load(a, row, u0 + U * (NB + i), ue, q);
-        }
-      }
+      for (int t = 0; t < NT; ++t) at[t] = xrow[t] + u * 256;
+      multiply<GROUP, 1, NT, U, Z>(cur, u, at, q, acc);
     }
+  };
+  // whole batches, then one that is cut short
+  const int whole = min(ue, a.n_in / 128), n = whole > ub ? (whole - ub) / U : 0;
+  int u0 = ub;
+  auto turn = [&]() {
+    compute();
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    put();
+    cur = next;
+    u0 += U;
+  };
+  if (ub < ue) {                                 // what is waited for first is requested first
+    if (n > 0) {
+      x.request(a, ub);
+      cur.load(a, row, ub, q);
+    } else {
+      x.request_last(a, ub);
+      cur.load_last(a, row, ub, ue, q);
+    }
+    put();
+    for (int i = 1; i < n; ++i) {
+      x.request(a, u0 + U);
+      next.load(a, row, u0 + U, q);
+      turn();
+    }
+    if (n > 0 && u0 + U < ue) {
+      x.request_last(a, u0 + U);
+      next.load_last(a, row, u0 + U, ue, q);
+      turn();
+    }
+    compute();
   }
   // the waves' sums, added in their order
   __syncthreads();
   f32x4* red = reinterpret_cast<f32x4*>(lds);
   if (w > 0) {
 #pragma unroll
-    for (int f = 0; f < RT; ++f)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) red[(((w - 1) * RT + f) * NT + t) * 64 + lane] = acc[f][t];
+    for (int t = 0; t < NT; ++t) red[((w - 1) * NT + t) * 64 + lane] = acc[0][t];
   }
   __syncthreads();
   if (w > 0) return;
 #pragma unroll
   for (int x = 0; x < KW - 1; ++x)
 #pragma unroll
-    for (int f = 0; f < RT; ++f)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[f][t] += red[((x * RT + f) * NT + t) * 64 + lane];
-  store_rows<E4M3, RT, NT>(a, n0, m, q, acc);
+    for (int t = 0; t < NT; ++t) acc[0][t] += red[(x * NT + t) * 64 + lane];
+  store_rows<E4M3, 1, NT>(a, n0, m, q, acc);
 }
 
-constexpr int proj_batch(int group) { return group == 32 ? 2 : 4; }      // (the scales of finer groups need the registers)
-
-// Many weight rows: every wave has 16 RT of its own and the whole reduction; the workgroup's waves share the staged rows of x, one part
-// in LDS while the next is on the way.
-template <int GROUP, int NT, int RT, bool E4M3>
+// Many weight rows: every wave has 16 RT of its own and the whole reduction; the workgroup's waves share the staged rows of x, U units
+// in LDS while the next are on the way.  P pieces of x per thread.
+template <int GROUP, int NT, int RT, int P, bool Z, bool E4M3>
 __global__ void __launch_bounds__(256, 2) proj_w4_kernel(const ProjArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  constexpr int kPieces = 8;                            // per thread and part: T * units * 16 <= 8 * 256
+  constexpr int U = proj_batch(GROUP, NT), kPitch = U * 256 + 16;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, q = lane >> 4;
   const int n0 = (blockIdx.x * 4 + w) * 16 * RT;
@@ -337,105 +353,117 @@ __global__ void __launch_bounds__(256, 2) proj_w4_kernel(const ProjArgs a) {
 #pragma unroll
   for (int f = 0; f < RT; ++f) row[f] = min(n0 + 16 * f + m, a.n_out - 1);
   const int nu = (a.n_in + 127) / 128;
-  constexpr int U = proj_batch(GROUP);
-  Batch<GROUP, RT, U> cur, next;
-  cur.load(a, row, 0, nu, q);
-  const int pitch = a.units * 256 + 16, all = a.T << a.shift;
-  Eight<E4M3> e[kPieces];
-  auto request = [&](int u0) {
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = threadIdx.x + 256 * j, t = i >> a.shift, k = u0 * 128 + 8 * (i - (t << a.shift));
-      e[j].load(a.x, (long long)t * a.n_in + k, i < all && k < a.n_in);
-    }
-  };
-  auto put = [&](unsigned char* to) {
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = threadIdx.x + 256 * j, t = i >> a.shift;
-      if (i < all) e[j].store(to + t * pitch + 16 * (i - (t << a.shift)));
-    }
-  };
-  request(0);
-  put(lds);
+  Staged<E4M3, U, 256, P> x;
+  x.init(a, threadIdx.x);
   f32x4 acc[RT][NT];
 #pragma unroll
   for (int f = 0; f < RT; ++f)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  __syncthreads();
-  int turn = 0;
-  for (int uc = 0; uc < nu; uc += a.units, turn ^= 1) {
-    const int cu = min(a.units, nu - uc);
-    const bool more = uc + a.units < nu;
-    if (more) request(uc + a.units);
+  Batch<GROUP, RT, U, Z> cur, next;
+  auto compute = [&](const unsigned char* from) {
     const unsigned char* xrow[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) xrow[t] = lds + (turn * a.T + min(16 * t + m, a.T - 1)) * pitch;
-    for (int u0 = uc; u0 < uc + cu; u0 += U) {
-      next.load(a, row, u0 + U, nu, q);
+    for (int t = 0; t < NT; ++t) xrow[t] = from + min(16 * t + m, a.T - 1) * kPitch;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (u0 + u < uc + cu) {                       // wave-uniform
-          const unsigned char* x[NT];
+    for (int u = 0; u < U; ++u) {
+      const unsigned char* at[NT];
 #pragma unroll
-          for (int t = 0; t < NT; ++t) x[t] = xrow[t] + (u0 - uc + u) * 256;
-          multiply<GROUP, RT, NT, U>(cur, u, a.zeros != nullptr, x, q, acc);
-        }
-      }
-      cur = next;
+      for (int t = 0; t < NT; ++t) at[t] = xrow[t] + u * 256;
+      multiply<GROUP, RT, NT, U, Z>(cur, u, at, q, acc);
     }
-    if (more) put(lds + (turn ^ 1) * a.T * pitch);
-    __syncthreads();
+  };
+  // whole batches, then one that is cut short
+  const int n = a.n_in / (128 * U);
+  unsigned char *from = lds, *to = lds + a.T * kPitch;
+  int u0 = 0;
+  auto turn = [&]() {
+    compute(from);
+    x.put(to);
+    __syncthreads();                      // everybody has read `from`, which is written next
+    cur = next;
+    unsigned char* const was = from;
+    from = to;
+    to = was;
+    u0 += U;
+  };
+  if (n > 0) {
+    x.request(a, 0);
+    cur.load(a, row, 0, q);
+  } else {
+    x.request_last(a, 0);
+    cur.load_last(a, row, 0, nu, q);
   }
+  x.put(lds);
+  __syncthreads();
+  for (int i = 1; i < n; ++i) {
+    x.request(a, u0 + U);
+    next.load(a, row, u0 + U, q);
+    turn();
+  }
+  if (n > 0 && u0 + U < nu) {
+    x.request_last(a, u0 + U);
+    next.load_last(a, row, u0 + U, nu, q);
+    turn();
+  }
+  compute(from);
   store_rows<E4M3, RT, NT>(a, n0, m, q, acc);
 }
 
-// Largest power of two of units, at least `batch`, whose T rows fit `bytes`; no more than it takes for `units`
-static void stage_units(ProjArgs& a, int batch, int bytes, int units) {
-  a.units = batch;
-  while (a.units < units && a.T * (2 * a.units * 256 + 16) <= bytes) a.units *= 2;
-  a.shift = log2_of(a.units * 16);
-}
-
-template <int GROUP, int NT, int RT, bool E4M3>
-static hipError_t go_many(ProjArgs& a, hipStream_t s) {
+template <int GROUP, int NT, int RT, int P, bool Z, bool E4M3>
+static hipError_t go_many(const ProjArgs& a, hipStream_t s) {
   static std::atomic<unsigned long long> allowed;
-  constexpr int kBytes = 8 * 256 * 16 + 32 * 16;          // staged rows, one part
-  stage_units(a, proj_batch(GROUP), kBytes, (a.n_in + 127) / 128);
-  auto kern = proj_w4_kernel<GROUP, NT, RT, E4M3>;
-  const hipError_t e = allow_lds(reinterpret_cast<const void*>(kern), 2 * kBytes, allowed);
+  constexpr int kPitch = proj_batch(GROUP, NT) * 256 + 16;
+  auto kern = proj_w4_kernel<GROUP, NT, RT, P, Z, E4M3>;
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(kern), 2 * 32 * kPitch, allowed);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((unsigned)((a.n_out + 64 * RT - 1) / (64 * RT))), dim3(256), 2 * a.T * (a.units * 256 + 16), s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((a.n_out + 64 * RT - 1) / (64 * RT))), dim3(256), 2 * a.T * kPitch, s, a);
   return hipGetLastError();
 }
 
-template <int GROUP, int NT, int RT, int KW, int NB, bool E4M3>
-static hipError_t go_split(ProjArgs& a, hipStream_t s) {
+template <int GROUP, int NT, int KW, int U, int P, bool Z, bool E4M3>
+static hipError_t go_split(const ProjArgs& a, hipStream_t s) {
   static std::atomic<unsigned long long> allowed;
-  // staged rows of a workgroup: two of them per compute unit, or, where that is less than two batches per wave, one
-  constexpr int kTwo = 72 * 1024, kOne = 144 * 1024;
-  const int least = a.T * (2 * 256 * NB + 16) * KW;
-  stage_units(a, 2 * NB, (least <= kTwo ? kTwo : kOne) / KW, ((a.n_in + 127) / 128 + KW - 1) / KW);
-  int bytes = KW * a.T * (a.units * 256 + 16);
-  if (bytes < (KW - 1) * RT * NT * 64 * 16) bytes = (KW - 1) * RT * NT * 64 * 16;
-  auto kern = proj_w4_split_kernel<GROUP, NT, RT, KW, NB, E4M3>;
-  const hipError_t e = allow_lds(reinterpret_cast<const void*>(kern), 160 * 1024, allowed);
+  constexpr int kPitch = U * 256 + 16;
+  int bytes = KW * a.T * kPitch;
+  if (bytes < (KW - 1) * NT * 64 * 16) bytes = (KW - 1) * NT * 64 * 16;
+  auto kern = proj_w4_split_kernel<GROUP, NT, KW, U, P, Z, E4M3>;
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(kern), KW * 16 * NT * kPitch, allowed);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((unsigned)((a.n_out + 16 * RT - 1) / (16 * RT))), dim3(64 * KW), bytes, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((a.n_out + 15) / 16)), dim3(64 * KW), bytes, s, a);
   return hipGetLastError();
 }
 
-template <int GROUP, int NT, bool E4M3>
-static hipError_t go_proj(ProjArgs& a, hipStream_t s) {
-  if (a.n_out >= 128 * 256) return go_many<GROUP, NT, 2, E4M3>(a, s);          // a workgroup or more of 128 rows per compute unit
-  return go_split<GROUP, NT, 1, 4, 2, E4M3>(a, s);
+// The form by size, each against the next best where the line is drawn (us; groups of 128, bf16 x; 32 rows: groups of 64 with zero points):
+//   shared staging      up to 4 rows of x never (65001 x 4096, one row: 26.8 split, 27.6); above, from 80 weight rows per compute unit on:
+//                       16 rows, 24576 x 4096 16.7 against 18.0, 12288 x 4096 15.6 against 10.9; 32 rows 27.6 against 33.8, 26.2 against 19.4.
+//                       Two blocks of 16 weight rows per wave where one would not fit the machine at once: 32 rows, 65001 x 4096 47.8 against
+//                       67.1, 49152 x 4096 45.6 against 42.3.
+//   eight waves along   where there are units enough and few weight rows or long ones: 4096 x 4096 5.1 against 5.7 (16 rows), 8.7 against 10.0
+//   the reduction       (32); 12288 x 1024 4.4 against 3.5 (one row).
+//   units per batch     as many as the registers for x leave: one row, 24576 x 4096 11.6 with four, 13.2 with two.
+template <int GROUP, bool Z, bool E4M3>
+static hipError_t go_proj(const ProjArgs& a, hipStream_t s) {
+  const int nu = (a.n_in + 127) / 128;
+  if (a.T > 4 && a.n_out >= 80 * 256) {
+    constexpr int P = proj_batch(GROUP, 1), P2 = proj_batch(GROUP, 2) * 2;          // pieces of x per thread for 16 and for 32 rows
+    if (a.n_out <= 3 * 64 * 256) return a.T <= 16 ? go_many<GROUP, 1, 1, P, Z, E4M3>(a, s) : go_many<GROUP, 2, 1, P2, Z, E4M3>(a, s);
+    return a.T <= 16 ? go_many<GROUP, 1, 2, P, Z, E4M3>(a, s) : go_many<GROUP, 2, 2, P2, Z, E4M3>(a, s);
+  }
+  if (nu >= 64 || (nu >= 32 && a.n_out <= 16 * 256)) {
+    if (a.T <= 4) return go_split<GROUP, 1, 8, 4, 4, Z, E4M3>(a, s);
+    if (a.T <= 8) return go_split<GROUP, 1, 8, 2, 4, Z, E4M3>(a, s);
+    return a.T <= 16 ? go_split<GROUP, 1, 8, 2, 8, Z, E4M3>(a, s) : go_split<GROUP, 2, 8, 1, 8, Z, E4M3>(a, s);
+  }
+  if (a.T <= 4 && nu >= 16) return go_split<GROUP, 1, 4, 4, 4, Z, E4M3>(a, s);
+  if (a.T <= 8) return go_split<GROUP, 1, 4, 2, 4, Z, E4M3>(a, s);
+  return a.T <= 16 ? go_split<GROUP, 1, 4, 2, 8, Z, E4M3>(a, s) : go_split<GROUP, 2, 4, 1, 8, Z, E4M3>(a, s);
 }
 
 template <int GROUP>
-static hipError_t go_proj(ProjArgs& a, bool e4m3, hipStream_t s) {
-  if (a.T <= 16) return e4m3 ? go_proj<GROUP, 1, true>(a, s) : go_proj<GROUP, 1, false>(a, s);
-  return e4m3 ? go_proj<GROUP, 2, true>(a, s) : go_proj<GROUP, 2, false>(a, s);
+static hipError_t go_proj(const ProjArgs& a, bool e4m3, hipStream_t s) {
+  if (a.zeros) return e4m3 ? go_proj<GROUP, true, true>(a, s) : go_proj<GROUP, true, false>(a, s);
+  return e4m3 ? go_proj<GROUP, false, true>(a, s) : go_proj<GROUP, false, false>(a, s);
 }
 
 hipError_t launch_proj_w4(const mohge_proj_config& c, const void* x, const float* x_scale, const void* codes,
