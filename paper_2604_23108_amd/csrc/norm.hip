@@ -3,6 +3,8 @@
 //   backward  n = h rstd, g = w dy, dx = ds + rstd (g - n mean(g n)),  dw = sum over rows of dy n
 // Bound by memory: a row is read once into registers (8 elements per thread and piece), its one or two sums
 // are folded across the threads that share it, and it is written from the registers.
+#include <type_traits>
+
 #include "block.h"
 
 namespace mohge {
@@ -134,18 +136,26 @@ hipError_t launch_rmsnorm(const mohge_norm_config& c, const void* x, const void*
 }
 
 // ---- backward -----------------------------------------------------------------------------------
-// A workgroup walks rows, gridDim.x apart, and keeps the part of dw of its rows in registers; its sums
-// go to the workspace, and a second kernel adds them in the order of the workgroups.
-constexpr int kBwdGroups = 512;
+// TPR threads share a row and walk rows, the next one's elements on the way while the sums of one are folded; a thread keeps the
+// part of dw of its columns in registers.  A workgroup's parts are added in LDS and left in the workspace, one row for
+// each workgroup, which a second kernel adds in their order.
+constexpr int kBwdGroups = 512;          // workgroups at most: two per compute unit
 
-template <bool BF16, int TPR, int NV>
-__global__ void __launch_bounds__(TPR) rmsnorm_bwd_kernel(const void* dy, const void* __restrict__ h,
-                                                          const float* __restrict__ weight,
-                                                          const float* __restrict__ rstd, const void* dsum, void* dx,
-                                                          float* __restrict__ partial, int T, int pieces, float inv_d) {
-  constexpr int kWaves = TPR / 64;
-  const int t = threadIdx.x, lane = t & 63;
-  __shared__ float red[2][kWaves];
+template <bool BF16, int NV>
+struct NormRow {
+  Piece<BF16> dy[NV], h[NV], ds[NV];
+  float rstd;
+};
+
+template <bool BF16, int TPR, int NV, bool DSUM>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_bwd_kernel(const void* dy, const void* __restrict__ h,
+                                                                            const float* __restrict__ weight,
+                                                                            const float* __restrict__ rstd, const void* dsum,
+                                                                            void* dx, float* __restrict__ partial, int T,
+                                                                            int pieces, float inv_d) {
+  constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kWaves = TPR / 64;
+  const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR, lane = threadIdx.x & 63;
+  __shared__ float red[2][kRows][kWaves];
   float w[NV][8], dw[NV][8];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -157,57 +167,85 @@ __global__ void __launch_bounds__(TPR) rmsnorm_bwd_kernel(const void* dy, const 
       b.get(w[i]);
     }
   }
-  int turn = 0;
-  for (int row = blockIdx.x; row < T; row += gridDim.x, turn ^= 1) {
+  // pieces past the row's end hold its last one, with a weight of 0
+  auto load = [&](NormRow<BF16, NV>& x, int row) {
     const long long base = (long long)row * pieces;
-    const float r = rstd[row];
+    x.rstd = rstd[row];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int p = min(t + i * TPR, pieces - 1);
+      x.dy[i].load(dy, base + p);
+      x.h[i].load(h, base + p);
+      if constexpr (DSUM) x.ds[i].load(dsum, base + p);
+    }
+  };
+  const int step = gridDim.x * kRows, row0 = blockIdx.x * kRows + mine;
+  const int turns = (T - (int)blockIdx.x * kRows + step - 1) / step;          // the same for the whole workgroup
+  NormRow<BF16, NV> cur, next;
+  load(cur, min(row0, T - 1));
+  for (int k = 0; k < turns; ++k) {
+    const int row = row0 + k * step;
+    if (k + 1 < turns) load(next, min(row + step, T - 1));
+    const float r = row < T ? cur.rstd : 0.f;
     float g[NV][8], n[NV][8], dot = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int p = t + i * TPR;
-      if (p < pieces) {
-        Piece<BF16> a, b;
-        a.load(dy, base + p);
-        b.load(h, base + p);
-        a.get(g[i]);
-        b.get(n[i]);
+      cur.dy[i].get(g[i]);
+      cur.h[i].get(n[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          n[i][j] *= r;
-          dw[i][j] = fmaf(g[i][j], n[i][j], dw[i][j]);
-          g[i][j] *= w[i][j];
-          dot = fmaf(g[i][j], n[i][j], dot);
-        }
+      for (int j = 0; j < 8; ++j) {
+        n[i][j] *= r;
+        if (row < T) dw[i][j] = fmaf(g[i][j], n[i][j], dw[i][j]);
+        g[i][j] *= w[i][j];
+        dot = fmaf(g[i][j], n[i][j], dot);
       }
     }
     dot = wave_sum(dot);
     if constexpr (kWaves > 1) {
-      if (lane == 0) red[turn][t >> 6] = dot;
+      if (lane == 0) red[k & 1][mine][t >> 6] = dot;
       __syncthreads();                       // two buffers: the next row's sums do not meet this row's reads
       dot = 0.f;
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) dot += red[turn][i];
+      for (int i = 0; i < kWaves; ++i) dot += red[k & 1][mine][i];
     }
     const float mean = dot * inv_d;
+    if (row < T) {
+      const long long base = (long long)row * pieces;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int p = t + i * TPR;
-      if (p < pieces) {
-        float o[8];
+      for (int i = 0; i < NV; ++i) {
+        if (t + i * TPR < pieces) {
+          float o[8], e[8];
+          if constexpr (DSUM) cur.ds[i].get(e);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = r * (g[i][j] - n[i][j] * mean);
-        Piece<BF16> a;
-        if (dsum) {
-          float e[8];
-          a.load(dsum, base + p);
-          a.get(e);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] += e[j];
+          for (int j = 0; j < 8; ++j) {
+            o[j] = r * (g[i][j] - n[i][j] * mean);
+            if constexpr (DSUM) o[j] += e[j];
+          }
+          Piece<BF16> a;
+          a.set(o);
+          a.store(dx, base + t + i * TPR);
         }
-        a.set(o);
-        a.store(dx, base + p);
       }
     }
+    cur = next;
+  }
+  // the rows' groups of a workgroup, added in their order
+  if constexpr (kRows > 1) {
+    __shared__ float sums[kRows - 1][NV * 8][TPR];
+    if (mine > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[mine - 1][8 * i + j][t] = dw[i][j];
+    }
+    __syncthreads();
+    if (mine > 0) return;
+#pragma unroll
+    for (int x = 0; x < kRows - 1; ++x)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] += sums[x][8 * i + j][t];
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -220,22 +258,39 @@ __global__ void __launch_bounds__(TPR) rmsnorm_bwd_kernel(const void* dy, const 
   }
 }
 
-// dw[j] = sum of n rows of the workspace: 64 columns per workgroup, 16 waves that stride the rows
-__global__ void __launch_bounds__(1024) rmsnorm_bwd_sum_kernel(const float* __restrict__ partial, float* dweight, int n,
-                                                               int d) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int j = blockIdx.x * 64 + lane;
-  float s = 0.f;
-  if (j < d)
-    for (int i = wv; i < n; i += 16) s += partial[(long long)i * d + j];
-  red[wv][lane] = s;
+// dw[j] = sum of n rows of the workspace: 32 columns per workgroup, four to a thread, 32 threads along the rows
+__global__ void __launch_bounds__(256) rmsnorm_bwd_sum_kernel(const float* __restrict__ partial, float* dweight, int n,
+                                                              int d) {
+  __shared__ float4 red[32][8];
+  const int c = threadIdx.x & 7, part = threadIdx.x >> 3, j = blockIdx.x * 32 + 4 * c;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (j < d) {
+#pragma unroll 8
+    for (int i = part; i < n; i += 32) {
+      const float4 v = *reinterpret_cast<const float4*>(partial + (long long)i * d + j);
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+  }
+  red[part][c] = s;
   __syncthreads();
-  if (wv == 0 && j < d) {
-    s = 0.f;
+  if (part < 4) {                                  // four threads add eight parts each, then one adds four
+    s = red[8 * part][c];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += red[i][lane];
-    dweight[j] = s;
+    for (int i = 1; i < 8; ++i) {
+      const float4 v = red[8 * part + i][c];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+  }
+  __syncthreads();
+  if (part < 4) red[part][c] = s;
+  __syncthreads();
+  if (part == 0 && j < d) {
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      const float4 v = red[i][c];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    *reinterpret_cast<float4*>(dweight + j) = s;
   }
 }
 
@@ -245,21 +300,31 @@ template <bool BF16>
 static hipError_t launch_norm_bwd(const mohge_norm_config& c, const void* dy, const void* h, const float* weight,
                                   const float* rstd, const void* dsum, void* dx, float* dweight, float* partial,
                                   hipStream_t s) {
-  const int pieces = c.d / 8, groups = c.T < kBwdGroups ? c.T : kBwdGroups;
-  auto go = [&](auto kern, int tpr) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(tpr), 0, s, dy, h, weight, rstd, dsum, dx, partial, c.T, pieces,
-                       1.f / c.d);
+  const int pieces = c.d / 8;
+  int groups = 0;
+  auto go = [&](auto tpr, auto nv) {
+    constexpr int kRows = tpr.value < 256 ? 256 / tpr.value : 1;
+    groups = (c.T + kRows - 1) / kRows;
+    if (groups > kBwdGroups) groups = kBwdGroups;
+    if (groups == 0) return;
+    auto launch = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(tpr.value < 256 ? 256 : tpr.value), 0, s, dy, h, weight, rstd, dsum,
+                         dx, partial, c.T, pieces, 1.f / c.d);
+    };
+    if (dsum) launch(rmsnorm_bwd_kernel<BF16, tpr.value, nv.value, true>);
+    else launch(rmsnorm_bwd_kernel<BF16, tpr.value, nv.value, false>);
   };
-  if (groups > 0) {
-    if (pieces <= 64) go(rmsnorm_bwd_kernel<BF16, 64, 1>, 64);
-    else if (pieces <= 128) go(rmsnorm_bwd_kernel<BF16, 128, 1>, 128);
-    else if (pieces <= 256) go(rmsnorm_bwd_kernel<BF16, 256, 1>, 256);
-    else if (pieces <= 512) go(rmsnorm_bwd_kernel<BF16, 256, 2>, 256);
-    else if (pieces <= 1024) go(rmsnorm_bwd_kernel<BF16, 512, 2>, 512);
-    else if (pieces <= 2048) go(rmsnorm_bwd_kernel<BF16, 1024, 2>, 1024);
-    else go(rmsnorm_bwd_kernel<BF16, 1024, 4>, 1024);
-  }
-  hipLaunchKernelGGL(rmsnorm_bwd_sum_kernel, dim3((unsigned)((c.d + 63) / 64)), dim3(1024), 0, s, partial, dweight, groups,
+  constexpr int kMost = BF16 ? 4 : 2;          // pieces that a thread's registers hold
+  auto with = [&](auto tpr) { go(tpr, std::integral_constant<int, kMost>()); };
+  if (pieces <= 64) go(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+  else if (pieces <= 128) go(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+  else if (pieces <= 64 * kMost) with(std::integral_constant<int, 64>());
+  else if (pieces <= 128 * kMost) with(std::integral_constant<int, 128>());
+  else if (pieces <= 256 * kMost) with(std::integral_constant<int, 256>());
+  else if (pieces <= 512 * kMost) with(std::integral_constant<int, 512>());
+  else if (pieces <= 1024 * 2) go(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+  else go(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+  hipLaunchKernelGGL(rmsnorm_bwd_sum_kernel, dim3((unsigned)((c.d + 31) / 32)), dim3(256), 0, s, partial, dweight, groups,
                      c.d);
   return hipGetLastError();
 }
