@@ -101,9 +101,12 @@ int mohge_cache_append(const mohge_cache_config* cfg, int32_t n_tokens, const vo
  * Out: out DEVICE [n_seqs, n_heads, head_size] (dtype); lse DEVICE [n_seqs, n_heads] f32 or NULL.
  * A sequence that is longer than its block table, or that has a page number outside 0..n_pages-1 among the pages
  * it reads, gets NaN (out and lse): a wrong number can never pass for a result.
- * workspace DEVICE, mohge_cache_workspace_size(cfg) bytes (never less for more sequences).
- * The axis is split over workgroups by the lengths found on the device; the parts are joined in a fixed
- * order (deterministic).
+ * workspace DEVICE, mohge_cache_workspace_size(cfg) bytes (a few MB, whatever the lengths; never less for more sequences).  It
+ * holds counters that MUST BE ZERO when the call starts and that the call leaves zero: clear it once (hipMemset) and keep
+ * it for calls of one cfg, issued in stream order; calls that overlap on one workspace race.  Were the counters not zero, results that
+ * are joined from parts stay NaN.
+ * The positions of all sequences are divided evenly over the workgroups, by the lengths found on the device; parts are
+ * joined in a fixed order (deterministic).
  */
 int mohge_cache_attention(const mohge_cache_config* cfg, const void* q, int64_t q_stride, const int32_t* block_table,
                           const int32_t* seq_lens, const void* k_pages, const void* v_pages, const float* k_scale,

@@ -36,6 +36,9 @@ int check_cache(const mohge_cache_config* c) {
   if (c->n_pages < 1 || c->max_pages < 1) { set_error("n_pages and max_pages must be positive"); return MOHGE_EINVAL; }
   if ((int64_t)c->max_pages * c->page_size >= (int64_t)1 << 31) {
     set_error("max_pages*page_size does not fit int32"); return MOHGE_EINVAL; }
+  // (the attention numbers its units of 64 positions or more in 32 bits)
+  if ((int64_t)c->n_seqs * c->n_heads * ((int64_t)c->max_pages * c->page_size / 64 + 1) >= (int64_t)1 << 31) {
+    set_error("n_seqs*n_heads*max_pages*page_size must be less than 2^37"); return MOHGE_EINVAL; }
   if (c->dtype != MOHGE_F32 && c->dtype != MOHGE_BF16) { set_error("dtype = %d unknown", c->dtype); return MOHGE_EINVAL; }
   if (c->cache_dtype != c->dtype && !(c->cache_dtype == MOHGE_E4M3 && c->dtype == MOHGE_BF16)) {
     set_error("cache_dtype = %d must be dtype, or MOHGE_E4M3 with MOHGE_BF16", c->cache_dtype); return MOHGE_EINVAL; }

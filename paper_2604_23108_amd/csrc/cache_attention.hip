@@ -15,6 +15,12 @@
 // The weights are split into two bf16 parts (the rest after the first is below 2^-17 of it), which costs one more
 // product and keeps them as good as fp32: one bf16 rounding of them would be as large as the output's own.
 // fp32 caches go through the fp32 matrix cores (16x16x4) with the same assignment, four positions at a time.
+//
+// Work split: the positions of every (sequence, kv head, block of 16 query heads) are cut into units of 128, one tile of 32 for each
+// wave, and the units of all of them, in one row, into equal stretches, one for each workgroup: whatever the lengths, every
+// workgroup has the same number of units.  The stretches follow from the lengths, which every workgroup reads for itself.
+// A row that lies in several stretches leaves parts (sums, maximum and total) in the workspace, and the workgroup that finishes last
+// joins them in their order.
 #include "block.h"
 
 namespace mohge {
@@ -38,10 +44,11 @@ struct AttArgs {
   const float* v_scale;
   void* out;
   float* lse;
-  float* part_o;              // [pieces][rows][D]
-  float2* part_ml;            // [pieces][rows]: maximum (of s log2 e) and sum
+  int32_t* done;              // [rows]: parts of a row that are complete; 0 between calls
+  float* part_o;              // [2 per workgroup][group of at most 16][D]
+  float2* part_ml;            // the same without D: maximum (of s log2 e) and sum
   float scale2;               // scale * log2 e
-  int n_seqs, n_heads, n_kv, group, page_shift, n_pages, max_pages, splits, chunk;
+  int n_seqs, n_heads, n_kv, group, page_shift, n_pages, max_pages;
 };
 
 __device__ __forceinline__ uint32_t cvt_bf16x2(uint32_t codes, bool hi) {
@@ -75,15 +82,17 @@ __device__ __forceinline__ void load_bytes(uint32_t* w, const unsigned char* p) 
 
 template <int CACHE, int D>
 struct AttTile {
+  // halves of 16 positions: two, but for the widest rows, whose second half would not fit the registers
+  static constexpr int H = CACHE == kCacheF32 && D == 256 ? 1 : 2;
   static constexpr int kBytes = CACHE == kCacheF32 ? 4 : CACHE == kCacheBf16 ? 2 : 1;
   static constexpr int kRow = D * kBytes;
   static constexpr int kKeyLoads = kRow / 64;             // 16 bytes per lane each, 64 bytes of a key's row
   static constexpr int kValBytes = kRow / 16;             // bytes of a value row per lane
   static constexpr int kQWords = CACHE == kCacheF32 ? D / 4 : D / 8;       // words of the query operand per lane
 
-  uint32_t k[2][kKeyLoads * 4];
-  uint32_t v[2][4][kValBytes / 4];
-  float ks[2][4], vs[2][4];
+  uint32_t k[H][kKeyLoads * 4];
+  uint32_t v[H][4][kValBytes / 4];
+  float ks[H][4], vs[H][4];
 
   // half hf of the tile lies in the page row `at` (rows of the page array)
   __device__ __forceinline__ void load(int hf, const AttArgs& a, long long at, int lane) {
@@ -141,11 +150,11 @@ struct AttTile {
     if constexpr (CACHE == kCacheE4m3) vs[hf][i] = 0.f;
   }
 
-  // o += V^T p for both halves
-  __device__ __forceinline__ void values(f32x4 (&o)[D / 16], const float (&p)[2][4]) const {
+  // o += V^T p for all halves
+  __device__ __forceinline__ void values(f32x4 (&o)[D / 16], const float (&p)[H][4]) const {
     if constexpr (CACHE == kCacheF32) {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
+      for (int hf = 0; hf < H; ++hf)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -218,203 +227,319 @@ __device__ __forceinline__ void store_out(void* out, long long at, const float* 
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
 
-// grid: sequences x kv heads x blocks of 16 query heads x splits
-template <int CACHE, int D>
-__global__ void __launch_bounds__(64 * kAttWaves) cache_attention_kernel(const AttArgs a) {
-  typedef AttTile<CACHE, D> Tile;
-  __shared__ float red_o[kAttWaves - 1][D / 4][64];
-  __shared__ float red_ml[kAttWaves - 1][2][64];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m = lane & 15, q = lane >> 4;
-  const int blocks = (a.group + 15) / 16;
-  const int split = blockIdx.x % a.splits, row = blockIdx.x / a.splits;
-  const int b = row / (a.n_kv * blocks), kv = row / blocks % a.n_kv, g0 = row % blocks * 16;
-  const bool there = g0 + m < a.group;
-  const int head = kv * a.group + g0 + m;
-  const int S = 1 << a.page_shift;
-  const int n = a.seq_lens[b];
-  const int len = min(n, a.max_pages << a.page_shift);
-  int bad = n > len;
-  const int begin = split * a.chunk, end = len - begin < a.chunk ? len : begin + a.chunk;
-  if (split > 0 && begin >= len) return;            // (the join takes the pieces that the length has)
-  const int32_t* table = a.block_table + (long long)b * a.max_pages;
+// a / b for a < 2^31, 0 < b
+__device__ __forceinline__ int udiv(int a, int b) { return (int)((unsigned)a / (unsigned)b); }
 
-  uint32_t qw[Tile::kQWords];
-  load_query<CACHE, D>(qw, a, b * a.q_stride + (long long)head * D, there, q);
-  f32x4 o[D / 16];
-#pragma unroll
-  for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float top = -INFINITY, sum = 0.f;
-
-  for (int t0 = begin + 32 * w; t0 < end; t0 += 32 * kAttWaves) {
-    Tile tile;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int h0 = t0 + 16 * hf < end ? t0 + 16 * hf : t0;        // a half past the end: read again, and masked
-      int page = table[h0 >> a.page_shift];
-      if ((unsigned)page >= (unsigned)a.n_pages) { page = 0; bad = 1; }
-      tile.load(hf, a, (((long long)page * a.n_kv + kv) << a.page_shift) + (h0 & (S - 1)), lane);
-    }
-    float s[2][4];
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const f32x4 z = tile.scores(hf, qw);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[hf][i] = z[i] * a.scale2;
-    }
-    if (t0 + 32 > end) {
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (t0 + 16 * hf + 4 * q + i >= end) {
-            s[hf][i] = -INFINITY;
-            tile.clear_values(hf, i);
-          }
-    }
-    float next = top;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) next = fmaxf(next, s[hf][i]);
-    next = fmaxf(next, __shfl_xor(next, 16, 64));
-    next = fmaxf(next, __shfl_xor(next, 32, 64));
-    const float ref = next == -INFINITY ? 0.f : next;
-    const float shrink = __builtin_amdgcn_exp2f(top - ref);
-    top = next;
-    float p[2][4];
-    sum *= shrink;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[hf][i] = __builtin_amdgcn_exp2f(s[hf][i] - ref);
-        sum += p[hf][i];
-      }
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) o[j] *= shrink;
-    tile.values(o, p);
-  }
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
-
-  // join of the waves, in their order
-  if (bad) sum = NAN;
-  if (w > 0) {
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) red_o[w - 1][4 * j + i][lane] = o[j][i];
-    red_ml[w - 1][0][lane] = top;
-    red_ml[w - 1][1][lane] = sum;
-  }
-  __syncthreads();
-  if (w > 0) return;
-  float all = top;
-#pragma unroll
-  for (int x = 0; x < kAttWaves - 1; ++x) all = fmaxf(all, red_ml[x][0][lane]);
-  const float ref = all == -INFINITY ? 0.f : all;
-  float f = __builtin_amdgcn_exp2f(top - ref);
-  sum *= f;
-#pragma unroll
-  for (int j = 0; j < D / 16; ++j) o[j] *= f;
-#pragma unroll
-  for (int x = 0; x < kAttWaves - 1; ++x) {
-    f = __builtin_amdgcn_exp2f(red_ml[x][0][lane] - ref);
-    sum = fmaf(f, red_ml[x][1][lane], sum);
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[j][i] = fmaf(f, red_o[x][4 * j + i][lane], o[j][i]);
-  }
-  if (!there) return;
-  // element (D/16) (4q + i) + j: D/16 in a row for every i
-  if (len <= a.chunk) {
-    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : NAN;
-    const long long at = ((long long)b * a.n_heads + head) * D + (D / 4) * q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < D / 16; j += 4) {
-        const float r[4] = {o[j][i] * inv, o[j + 1][i] * inv, o[j + 2][i] * inv, o[j + 3][i] * inv};
-        store_out<CACHE>(a.out, at + (D / 16) * i + j, r);
-      }
-    if (a.lse && q == 0) a.lse[(long long)b * a.n_heads + head] = (ref + log2f(sum)) * (1.f / kLog2e);
-  } else {
-    const long long piece = ((long long)b * a.n_heads + head) * a.splits + split;
-    float* to = a.part_o + piece * D + (D / 4) * q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < D / 16; j += 4)
-        *reinterpret_cast<float4*>(to + (D / 16) * i + j) = make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]);
-    if (q == 0) a.part_ml[piece] = make_float2(all, sum);
-  }
+// Units of a sequence: at least one, which writes the result of an empty one
+template <int UNIT>
+__device__ __forceinline__ int units_of(const AttArgs& a, int b) {
+  const int len = min(max(a.seq_lens[b], 0), a.max_pages << a.page_shift);
+  return len > 0 ? (len + UNIT - 1) / UNIT : 1;
 }
 
-// The pieces of one (sequence, head), joined in their order: D/4 threads with 4 elements each
-template <int CACHE, int D>
-__global__ void __launch_bounds__(64) cache_attention_join_kernel(const AttArgs a) {
-  const int row = blockIdx.x, b = row / a.n_heads;
-  const int len = min(a.seq_lens[b], a.max_pages << a.page_shift);
-  if (len <= a.chunk) return;
-  const int pieces = (len + a.chunk - 1) / a.chunk;
-  const float2* ml = a.part_ml + (long long)row * a.splits;
-  const float* po = a.part_o + (long long)row * a.splits * D;
-  float all = -INFINITY;
-  for (int p = 0; p < pieces; ++p) all = fmaxf(all, ml[p].x);
-  const float ref = all == -INFINITY ? 0.f : all;
-  float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  const int e = threadIdx.x * 4;
-  if (e >= D) return;
-  for (int p = 0; p < pieces; ++p) {
-    const float f = __builtin_amdgcn_exp2f(ml[p].x - ref);
-    const float4 v = *reinterpret_cast<const float4*>(po + (long long)p * D + e);
-    sum = fmaf(f, ml[p].y, sum);
-    o[0] = fmaf(f, v.x, o[0]); o[1] = fmaf(f, v.y, o[1]); o[2] = fmaf(f, v.z, o[2]); o[3] = fmaf(f, v.w, o[3]);
-  }
-  const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : NAN;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] *= inv;
-  store_out<CACHE>(a.out, (long long)row * D + e, o);
-  if (a.lse && threadIdx.x == 0) a.lse[row] = (ref + log2f(sum)) * (1.f / kLog2e);
+// Stores that go through the XCD's cache, so that a workgroup on any XCD reads them once they are complete
+__device__ __forceinline__ void store_through(float2* p, const float2 v) {
+  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
 }
-
-// Pieces of `chunk` positions per sequence
-static void cache_splits(const mohge_cache_config& c, int& splits, int& chunk) {
-  const int step = 32 * kAttWaves;
-  const int longest = c.max_pages * c.page_size;
-  const long long rows = (long long)(c.n_seqs > 0 ? c.n_seqs : 1) * c.n_kv_heads * ((c.n_heads / c.n_kv_heads + 15) / 16);
-  long long want = (1024 + rows - 1) / rows;
-  const long long most = (longest + step - 1) / step;
-  if (want > most) want = most;
-  if (want < 1) want = 1;
-  chunk = (int)((longest + want - 1) / want);
-  chunk = (chunk + step - 1) / step * step;
-  splits = (longest + chunk - 1) / chunk;
+__device__ __forceinline__ void store_through(float* p, const float4 v) {
+  store_through(reinterpret_cast<float2*>(p), make_float2(v.x, v.y));
+  store_through(reinterpret_cast<float2*>(p) + 1, make_float2(v.z, v.w));
 }
-
-size_t cache_workspace_bytes(const mohge_cache_config& c) {
-  int splits, chunk;
-  cache_splits(c, splits, chunk);
-  const size_t pieces = (size_t)c.n_seqs * c.n_heads * splits;
-  return splits > 1 ? pieces * (c.head_size * sizeof(float) + sizeof(float2)) : 0;
-}
-
-template <int CACHE, int D>
-static void go_attention(const AttArgs& a, hipStream_t s) {
-  const int blocks = (a.group + 15) / 16;
-  hipLaunchKernelGGL((cache_attention_kernel<CACHE, D>), dim3((unsigned)(a.n_seqs * a.n_kv * blocks * a.splits)), dim3(64 * kAttWaves), 0,
-                     s, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL((cache_attention_join_kernel<CACHE, D>), dim3(a.n_seqs * a.n_heads), dim3(64), 0, s, a);
+__device__ __forceinline__ void store_through(float* p, const float v) {
+  __hip_atomic_store(reinterpret_cast<unsigned*>(p), __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 template <int CACHE>
-static void go_attention(const AttArgs& a, int D, hipStream_t s) {
-  if (D == 64) go_attention<CACHE, 64>(a, s);
-  else if (D == 128) go_attention<CACHE, 128>(a, s);
-  else go_attention<CACHE, 256>(a, s);
+__device__ __forceinline__ void finish_row(const AttArgs& a, long long head, float ref, float sum) {
+  if (a.lse) a.lse[head] = (ref + log2f(sum)) * (1.f / kLog2e);
+}
+
+// What a row's sums are multiplied by: 0 for a row without weight; NaN stays
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+
+template <int CACHE, int D, int OCC>
+__global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(const AttArgs a) {
+  typedef AttTile<CACHE, D> Tile;
+  constexpr int H = Tile::H, kTile = 16 * H, kUnit = kTile * kAttWaves;
+  constexpr int kOutBytes = CACHE == kCacheF32 ? 4 : 2;
+  __shared__ float red_o[kAttWaves - 1][D / 4][64];
+  __shared__ float red_ml[kAttWaves - 1][2][64];
+  __shared__ int last;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = lane & 15, q = lane >> 4;
+  const int blocks = (a.group + 15) / 16, rows = a.n_kv * blocks, gmax = min(a.group, 16);
+  const int S = 1 << a.page_shift;
+
+  // units of all sequences, and this workgroup's stretch [u, u_end)
+  int mine = lane < a.n_seqs ? units_of<kUnit>(a, lane) : 0;          // of sequences base .. base + 63
+  int upto = wave_incl_scan(mine), base = 0;
+  int total = __builtin_amdgcn_readlane(upto, 63);
+  for (int b0 = 64; b0 < a.n_seqs; b0 += 64)
+    total += __builtin_amdgcn_readlane(wave_incl_scan(b0 + lane < a.n_seqs ? units_of<kUnit>(a, b0 + lane) : 0), 63);
+  total *= rows;
+  const int per = udiv(total + (int)gridDim.x - 1, gridDim.x);
+  int u = (int)blockIdx.x * per;
+  const int u_end = min(u + per, total);
+  if (u >= total) return;
+  int before = 0;                                 // units (of one row) in front of sequence `base`
+  while (u < u_end) {
+    // the sequence of unit u, its row and its place in the row
+    unsigned long long hit;
+    while (!(hit = __ballot((long long)(before + upto) * rows > u))) {
+      before += __builtin_amdgcn_readlane(upto, 63);
+      base += 64;
+      mine = base + lane < a.n_seqs ? units_of<kUnit>(a, base + lane) : 0;
+      upto = wave_incl_scan(mine);
+    }
+    const int at = (int)__builtin_ctzll(hit), b = base + at;
+    const int units = __builtin_amdgcn_readlane(mine, at);
+    const int first = (before + __builtin_amdgcn_readlane(upto, at) - units) * rows;          // unit 0 of the sequence's row 0
+    const int row = udiv(u - first, units), start = u - first - row * units;
+    const int n_units = min(units - start, u_end - u);
+    const int kv = udiv(row, blocks), g0 = (row - kv * blocks) * 16;
+    const bool there = g0 + m < a.group;
+    const int head = kv * a.group + g0 + m;
+    const int n = a.seq_lens[b];
+    const int len = min(max(n, 0), a.max_pages << a.page_shift);
+    int bad = n > len;
+
+    const int32_t* table = a.block_table + (long long)b * a.max_pages;
+    uint32_t qw[Tile::kQWords];
+    load_query<CACHE, D>(qw, a, b * a.q_stride + (long long)head * D, there, q);
+    f32x4 o[D / 16];
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, sum = 0.f;
+
+    // this wave's tiles: kUnit apart from p0 on, those in front of p_end
+    const int p0 = start * kUnit + w * kTile, p_end = min(len, (start + n_units) * kUnit);
+    const int tiles = p_end > p0 ? (p_end - p0 + kUnit - 1) / kUnit : 0;
+    constexpr int kAhead = 64 / H;                 // tiles whose pages a wave looks up together, one half per lane
+    int pages = 0;
+    auto look_up = [&](int t0) {
+      const int pos = p0 + (t0 + lane / H) * kUnit + 16 * (lane % H);
+      const bool in = pos < p_end && t0 + lane / H < tiles;
+      pages = in ? table[pos >> a.page_shift] : 0;
+      if (__ballot((unsigned)pages >= (unsigned)a.n_pages)) bad = 1;
+      if ((unsigned)pages >= (unsigned)a.n_pages) pages = 0;
+    };
+    auto load = [&](Tile& tile, int t) {
+#pragma unroll
+      for (int hf = 0; hf < H; ++hf) {
+        const int pos = p0 + t * kUnit + 16 * hf;
+        const int half = pos < p_end ? hf : 0;                    // a half past the end: read the first again, and mask it
+        const long long page = __builtin_amdgcn_readlane(pages, (t % kAhead) * H + half);
+        tile.load(hf, a, ((page * a.n_kv + kv) << a.page_shift) + ((pos - 16 * (hf - half)) & (S - 1)), lane);
+      }
+    };
+    auto compute = [&](Tile& tile, int t) {
+      const int pos = p0 + t * kUnit;
+      float s[H][4];
+#pragma unroll
+      for (int hf = 0; hf < H; ++hf) {
+        const f32x4 z = tile.scores(hf, qw);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[hf][i] = z[i] * a.scale2;
+      }
+      if (pos + kTile > p_end) {
+#pragma unroll
+        for (int hf = 0; hf < H; ++hf)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (pos + 16 * hf + 4 * q + i >= p_end) {
+              s[hf][i] = -INFINITY;
+              tile.clear_values(hf, i);
+            }
+      }
+      float next = top;
+#pragma unroll
+      for (int hf = 0; hf < H; ++hf)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) next = fmaxf(next, s[hf][i]);
+      next = fmaxf(next, __shfl_xor(next, 16, 64));
+      next = fmaxf(next, __shfl_xor(next, 32, 64));
+      const float ref = next == -INFINITY ? 0.f : next;
+      const float shrink = __builtin_amdgcn_exp2f(top - ref);
+      top = next;
+      sum *= shrink;
+      float p[H][4];
+#pragma unroll
+      for (int hf = 0; hf < H; ++hf)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[hf][i] = __builtin_amdgcn_exp2f(s[hf][i] - ref);
+          sum += p[hf][i];
+        }
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o[j] *= shrink;
+      tile.values(o, p);
+    };
+    if (tiles > 0) {
+      // one tile on the way while the one before is multiplied
+      Tile cur, next;
+      look_up(0);
+      load(cur, 0);
+      int t = 0;
+      for (; t + 1 < tiles; ++t) {
+        if ((t + 1) % kAhead == 0) look_up(t + 1);
+        load(next, t + 1);
+        compute(cur, t);
+        cur = next;
+      }
+      compute(cur, t);
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+
+    // join of the waves, in their order
+    if (bad) sum = NAN;
+    if (w > 0) {
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red_o[w - 1][4 * j + i][lane] = o[j][i];
+      red_ml[w - 1][0][lane] = top;
+      red_ml[w - 1][1][lane] = sum;
+    }
+    __syncthreads();
+    const bool whole = n_units == units;
+    const int slot = 2 * blockIdx.x + (start == 0);
+    if (w == 0) {
+      float all = top;
+#pragma unroll
+      for (int x = 0; x < kAttWaves - 1; ++x) all = fmaxf(all, red_ml[x][0][lane]);
+      const float ref = all == -INFINITY ? 0.f : all;
+      float f = __builtin_amdgcn_exp2f(top - ref);
+      sum *= f;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o[j] *= f;
+#pragma unroll
+      for (int x = 0; x < kAttWaves - 1; ++x) {
+        f = __builtin_amdgcn_exp2f(red_ml[x][0][lane] - ref);
+        sum = fmaf(f, red_ml[x][1][lane], sum);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[j][i] = fmaf(f, red_o[x][4 * j + i][lane], o[j][i]);
+      }
+      // element (D/16) (4q + i) + j: D/16 in a row for every i
+      if (there) {
+        if (whole) {
+          const float inv = inverse(sum);
+          const long long to = ((long long)b * a.n_heads + head) * D + (D / 4) * q;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < D / 16; j += 4) {
+              const float r[4] = {o[j][i] * inv, o[j + 1][i] * inv, o[j + 2][i] * inv, o[j + 3][i] * inv};
+              store_out<CACHE>(a.out, to + (D / 16) * i + j, r);
+            }
+          if (q == 0) finish_row<CACHE>(a, (long long)b * a.n_heads + head, ref, sum);
+        } else {
+          float* to = a.part_o + ((long long)slot * gmax + m) * D + (D / 4) * q;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < D / 16; j += 4)
+              store_through(to + (D / 16) * i + j, make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]));
+          if (q == 0) store_through(a.part_ml + (long long)slot * gmax + m, make_float2(all, sum));
+        }
+      }
+      if (!whole) {
+        // the row's parts are complete where the last one is counted
+        const int r0 = first + row * units, parts = udiv(r0 + units - 1, per) - udiv(r0, per) + 1;
+        // (until then the result is NaN: if the counters were not 0 at the start, nothing can pass for a result)
+        if (there && start == 0) {
+          const float nan = __uint_as_float(0x7fc07fc0u);          // also as two bf16 numbers
+          unsigned char* to = static_cast<unsigned char*>(a.out) + (((long long)b * a.n_heads + head) * D + (D / 4) * q) * kOutBytes;
+#pragma unroll
+          for (int i = 0; i < D / 4 * kOutBytes; i += 16)
+            store_through(reinterpret_cast<float*>(to + i), make_float4(nan, nan, nan, nan));
+          if (a.lse && q == 0) store_through(a.lse + (long long)b * a.n_heads + head, nan);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (lane == 0) {
+          int32_t* const done = a.done + (long long)b * rows + row;
+          const int old = __hip_atomic_fetch_add(done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          if (old == parts - 1) __hip_atomic_store(done, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          last = old == parts - 1;
+        }
+      }
+    }
+    __syncthreads();
+    if (!whole && last) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+      // parts in the order of their workgroups: the first is that workgroup's second slot, the others their first.  Threads take
+      // four elements of a head each, as many threads as there are left share its parts.
+      const int r0 = first + row * units, w0 = udiv(r0, per), parts = udiv(r0 + units - 1, per) - w0 + 1;
+      const int heads = min(16, a.group - g0);
+      auto slot_of = [&](int p) { return 2 * (w0 + p) + (p == 0); };
+      for (int h = w; h < heads; h += kAttWaves) {             // a wave per head: 64 lanes = D/4 elements x 64 / (D/4) shares of the parts
+        constexpr int kLanes = D / 4, kShares = 64 / kLanes;
+        const int e = lane % kLanes * 4, share = lane / kLanes;
+        float all = -INFINITY;
+        for (int p = lane; p < parts; p += 64) all = fmaxf(all, a.part_ml[(long long)slot_of(p) * gmax + h].x);
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) all = fmaxf(all, __shfl_xor(all, off, 64));
+        const float ref = all == -INFINITY ? 0.f : all;
+        float l = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int p = share; p < parts; p += kShares) {
+          const long long sl = (long long)slot_of(p) * gmax + h;
+          const float2 ml = a.part_ml[sl];
+          const float4 v = *reinterpret_cast<const float4*>(a.part_o + sl * D + e);
+          const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+          l = fmaf(f, ml.y, l);
+          r[0] = fmaf(f, v.x, r[0]); r[1] = fmaf(f, v.y, r[1]); r[2] = fmaf(f, v.z, r[2]); r[3] = fmaf(f, v.w, r[3]);
+        }
+#pragma unroll
+        for (int off = kLanes; off < 64; off <<= 1) {
+          l += __shfl_xor(l, off, 64);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] += __shfl_xor(r[i], off, 64);
+        }
+        const float inv = inverse(l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] *= inv;
+        const long long hd = (long long)b * a.n_heads + kv * a.group + g0 + h;
+        if (share == 0) store_out<CACHE>(a.out, hd * D + e, r);
+        if (lane == 0) finish_row<CACHE>(a, hd, ref, l);
+      }
+    }
+    u += n_units;
+  }
+}
+
+// Waves per SIMD that the registers of a form allow (two tiles and the sums of one)
+constexpr int att_waves(int cache, int d) {
+  return cache == kCacheF32 ? (d == 64 ? 2 : 1) : cache == kCacheBf16 ? (d == 64 ? 3 : d == 128 ? 2 : 1) : d == 64 ? 3 : d == 128 ? 2 : 1;
+}
+
+static int att_rows(const mohge_cache_config& c) { return c.n_kv_heads * ((c.n_heads / c.n_kv_heads + 15) / 16); }
+
+// Workgroups: as many as are resident at once, no more than there can be units
+static int att_groups(const mohge_cache_config& c) {
+  const int cache = c.cache_dtype == MOHGE_F32 ? kCacheF32 : c.cache_dtype == MOHGE_BF16 ? kCacheBf16 : kCacheE4m3;
+  const int unit = (cache == kCacheF32 && c.head_size == 256 ? 16 : 32) * kAttWaves;
+  const long long units = (long long)c.n_seqs * att_rows(c) * (((long long)c.max_pages * c.page_size + unit - 1) / unit);
+  const long long most = 256 * att_waves(cache, c.head_size);
+  return (int)(units < most ? units : most);
+}
+
+static size_t att_done_bytes(const mohge_cache_config& c) { return ((size_t)c.n_seqs * att_rows(c) * sizeof(int32_t) + 255) / 256 * 256; }
+
+size_t cache_workspace_bytes(const mohge_cache_config& c) {
+  const int group = c.n_heads / c.n_kv_heads, gmax = group < 16 ? group : 16;
+  return att_done_bytes(c) + (size_t)att_groups(c) * 2 * gmax * (c.head_size * sizeof(float) + sizeof(float2));
+}
+
+template <int CACHE>
+static void go_attention(const AttArgs& a, int D, int groups, hipStream_t s) {
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(64 * kAttWaves), 0, s, a); };
+  if (D == 64) go(cache_attention_kernel<CACHE, 64, att_waves(CACHE, 64)>);
+  else if (D == 128) go(cache_attention_kernel<CACHE, 128, att_waves(CACHE, 128)>);
+  else go(cache_attention_kernel<CACHE, 256, att_waves(CACHE, 256)>);
 }
 
 hipError_t launch_cache_attention(const mohge_cache_config& c, const void* q, long long q_stride,
@@ -427,12 +552,13 @@ hipError_t launch_cache_attention(const mohge_cache_config& c, const void* q, lo
   a.out = out; a.lse = lse; a.scale2 = scale * kLog2e;
   a.n_seqs = c.n_seqs; a.n_heads = c.n_heads; a.n_kv = c.n_kv_heads; a.group = c.n_heads / c.n_kv_heads;
   a.page_shift = log2_of(c.page_size); a.n_pages = c.n_pages; a.max_pages = c.max_pages;
-  cache_splits(c, a.splits, a.chunk);
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)c.n_seqs * c.n_heads * a.splits * c.head_size);
-  if (c.cache_dtype == MOHGE_F32) go_attention<kCacheF32>(a, c.head_size, s);
-  else if (c.cache_dtype == MOHGE_BF16) go_attention<kCacheBf16>(a, c.head_size, s);
-  else go_attention<kCacheE4m3>(a, c.head_size, s);
+  const int groups = att_groups(c), gmax = a.group < 16 ? a.group : 16;
+  a.done = static_cast<int32_t*>(ws);
+  a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + att_done_bytes(c));
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)groups * 2 * gmax * c.head_size);
+  if (c.cache_dtype == MOHGE_F32) go_attention<kCacheF32>(a, c.head_size, groups, s);
+  else if (c.cache_dtype == MOHGE_BF16) go_attention<kCacheBf16>(a, c.head_size, groups, s);
+  else go_attention<kCacheE4m3>(a, c.head_size, groups, s);
   return hipGetLastError();
 }
 

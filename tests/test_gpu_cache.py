@@ -82,12 +82,14 @@ def _attend(cfg, lens, seed=0, scale=None):
     shape = (cfg.n_seqs, cfg.n_heads, cfg.head_size)
     out = g.wrap(torch.empty(shape, dtype=TYPES[cfg.dtype], device="cuda"), "out").fill_(float("nan"))
     lse = g.wrap(torch.empty(shape[:2], device="cuda"), "lse").fill_(float("nan"))
-    ws = g.wrap(torch.empty(max(16, M.mohge_cache_workspace_size(cfg)), dtype=torch.uint8, device="cuda"), "workspace")
+    ws = g.wrap(torch.empty(max(16, M.mohge_cache_workspace_size(cfg)), dtype=torch.uint8, device="cuda"), "workspace").zero_()
     scale = cfg.head_size ** -0.5 if scale is None else scale
     q, table, sl, kp, vp, ks, vs = args
     M.mohge_cache_attention(cfg, q, table, sl, kp, vp, ks, vs, scale, out, lse, ws)
     _check(cfg, *args, scale, out, lse)
     g.check()
+    blocks = cfg.n_kv_heads * -(-(cfg.n_heads // cfg.n_kv_heads) // 16)
+    assert (ws[:4 * cfg.n_seqs * blocks] == 0).all()              # the counters, for the next call
     return args, out, lse, ws
 
 
@@ -172,6 +174,18 @@ def test_pages_out_of_range_give_nan_and_touch_no_other_sequence(dtype, cache):
     long[2] = -5
     M.mohge_cache_attention(cfg, q, table, long, kp, vp, ks, vs, 128 ** -0.5, out, lse, ws)
     assert (out[2] == 0).all() and (lse[2] == -math.inf).all() and torch.equal(out[[0, 1, 3]], good[[0, 1, 3]])
+
+
+def test_counters_that_were_not_zero_leave_nan():
+    cfg = M.CacheConfig(2, 8, 2, 128, 16, 800, 600)
+    (q, table, lens, kp, vp, ks, vs), out, lse, ws = _attend(cfg, [9000, 40], 6)
+    good = out.clone()
+    ws[:16] = 77
+    M.mohge_cache_attention(cfg, q, table, lens, kp, vp, ks, vs, 128 ** -0.5, out, lse, ws)
+    assert out[0].isnan().all() and lse[0].isnan().all() and torch.equal(out[1], good[1])
+    ws.zero_()
+    M.mohge_cache_attention(cfg, q, table, lens, kp, vp, ks, vs, 128 ** -0.5, out, lse, ws)
+    assert torch.equal(out, good)
 
 
 @pytest.mark.parametrize("dtype,cache", KINDS)
