@@ -45,8 +45,8 @@ struct AttArgs {
   void* out;
   float* lse;
   int32_t* done;              // [rows]: parts of a row that are complete; 0 between calls
-  float* part_o;              // [2 per workgroup][group of at most 16][D]
-  float2* part_ml;            // the same without D: maximum (of s log2 e) and sum
+  float2* part_o;             // [2 per workgroup][D / 8][4][heads of a row]: pairs of a lane's elements, lane after lane
+  float2* part_ml;            // [2 per workgroup][heads of a row]: maximum (of s log2 e) and sum
   float scale2;               // scale * log2 e
   int n_seqs, n_heads, n_kv, group, page_shift, n_pages, max_pages;
 };
@@ -242,21 +242,37 @@ __device__ __forceinline__ void store_through(float2* p, const float2 v) {
   __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED,
                      __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ void store_through(float* p, const float4 v) {
-  store_through(reinterpret_cast<float2*>(p), make_float2(v.x, v.y));
-  store_through(reinterpret_cast<float2*>(p) + 1, make_float2(v.z, v.w));
+// ... and loads that see them.  (An acquiring fence instead makes every wave that joins invalidate its XCD's cache.)
+__device__ __forceinline__ float2 load_through(const float2* p) {
+  return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT));
 }
 __device__ __forceinline__ void store_through(float* p, const float v) {
   __hip_atomic_store(reinterpret_cast<unsigned*>(p), __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <int CACHE>
-__device__ __forceinline__ void finish_row(const AttArgs& a, long long head, float ref, float sum) {
-  if (a.lse) a.lse[head] = (ref + log2f(sum)) * (1.f / kLog2e);
-}
+// Stretches of `per` units begin at multiples of it, except in rows that are short or hardly longer than a stretch: those are not cut, a
+// stretch begins at their nearer end.  (A part has to be written, counted and read again: 464 rows of 8 units in stretches
+// of 5 take 20.8 us cut and 17.6 whole, 32 rows of 4 units 12.0 and 9.5.)
+template <int SHORT>
+struct Stretches {
+  int per;
+  __device__ __forceinline__ bool keep_whole(int units) const {
+    return units <= SHORT || (units >= per && units <= per + max(1, per / 2));
+  }
+  // unit v, which is unit `start` of a row of `units`
+  __device__ __forceinline__ int begin(int v, int start, int units) const {
+    return !keep_whole(units) ? v : 2 * start <= units ? v - start : v + units - start;
+  }
+  // the stretches that hold the first and the last unit of a row that is cut, which begins at unit r0
+  __device__ __forceinline__ int first_of(int r0) const { return udiv(r0, per); }
+  __device__ __forceinline__ int last_of(int r0, int units) const { return udiv(r0 + units - 1, per); }
+};
 
-// What a row's sums are multiplied by: 0 for a row without weight; NaN stays
-__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+// A row of which this workgroup has a part
+struct Part {
+  int b, row, first, parts;          // sequence, row of it, first workgroup, workgroups
+};
 
 template <int CACHE, int D, int OCC>
 __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(const AttArgs a) {
@@ -265,7 +281,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
   constexpr int kOutBytes = CACHE == kCacheF32 ? 4 : 2;
   __shared__ float red_o[kAttWaves - 1][D / 4][64];
   __shared__ float red_ml[kAttWaves - 1][2][64];
-  __shared__ int last;
+  __shared__ int last[2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, q = lane >> 4;
   const int blocks = (a.group + 15) / 16, rows = a.n_kv * blocks, gmax = min(a.group, 16);
@@ -278,24 +294,96 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
   for (int b0 = 64; b0 < a.n_seqs; b0 += 64)
     total += __builtin_amdgcn_readlane(wave_incl_scan(b0 + lane < a.n_seqs ? units_of<kUnit>(a, b0 + lane) : 0), 63);
   total *= rows;
-  const int per = udiv(total + (int)gridDim.x - 1, gridDim.x);
-  int u = (int)blockIdx.x * per;
-  const int u_end = min(u + per, total);
-  if (u >= total) return;
+  // (two units at least where rows are long: with one, more parts are joined than it helps)
+  Stretches<CACHE == kCacheF32 ? 1 : 4> cut;          // (an fp32 unit takes as long as a part costs)
+  cut.per = max(udiv(total + (int)gridDim.x - 1, gridDim.x), total >= 8ll * a.n_seqs * rows ? 2 : 1);
   int before = 0;                                 // units (of one row) in front of sequence `base`
-  while (u < u_end) {
-    // the sequence of unit u, its row and its place in the row
+  // the sequence b of unit v (at least as far as the last one asked for), its row, the unit's place in the row
+  int b, units, first, row, start;
+  auto locate = [&](int v) {
     unsigned long long hit;
-    while (!(hit = __ballot((long long)(before + upto) * rows > u))) {
+    while (!(hit = __ballot((long long)(before + upto) * rows > v))) {
       before += __builtin_amdgcn_readlane(upto, 63);
       base += 64;
       mine = base + lane < a.n_seqs ? units_of<kUnit>(a, base + lane) : 0;
       upto = wave_incl_scan(mine);
     }
-    const int at = (int)__builtin_ctzll(hit), b = base + at;
-    const int units = __builtin_amdgcn_readlane(mine, at);
-    const int first = (before + __builtin_amdgcn_readlane(upto, at) - units) * rows;          // unit 0 of the sequence's row 0
-    const int row = udiv(u - first, units), start = u - first - row * units;
+    const int at = (int)__builtin_ctzll(hit);
+    b = base + at;
+    units = __builtin_amdgcn_readlane(mine, at);
+    first = (before + __builtin_amdgcn_readlane(upto, at) - units) * rows;          // unit 0 of the sequence's row 0
+    row = udiv(v - first, units);
+    start = v - first - row * units;
+  };
+  auto begin_of = [&](int i) {
+    if ((long long)i * cut.per >= total) return total;
+    locate(i * cut.per);
+    return cut.begin(i * cut.per, start, units);
+  };
+  int u = begin_of(blockIdx.x);
+  const int base0 = base, before0 = before, mine0 = mine, upto0 = upto;
+  const int u_end = begin_of(blockIdx.x + 1);
+  if (u >= u_end) return;
+  base = base0; before = before0; mine = mine0; upto = upto0;
+  Part part[2];                                   // (the first row and the last one)
+  int n_parts = 0;
+  const int pitch = 4 * gmax, mine_at = q * gmax + m;
+  f32x4 o[D / 16];
+  float top, sum;
+  // the waves' sums, joined by the first in their order
+  auto join_waves = [&]() {
+    if (w > 0) {
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red_o[w - 1][4 * j + i][lane] = o[j][i];
+      red_ml[w - 1][0][lane] = top;
+      red_ml[w - 1][1][lane] = sum;
+    }
+    __syncthreads();
+    if (w == 0) {
+      float all = top;
+#pragma unroll
+      for (int x = 0; x < kAttWaves - 1; ++x) all = fmaxf(all, red_ml[x][0][lane]);
+      const float ref = all == -INFINITY ? 0.f : all;
+      float f = __builtin_amdgcn_exp2f(top - ref);
+      sum *= f;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o[j] *= f;
+#pragma unroll
+      for (int x = 0; x < kAttWaves - 1; ++x) {
+        f = __builtin_amdgcn_exp2f(red_ml[x][0][lane] - ref);
+        sum = fmaf(f, red_ml[x][1][lane], sum);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[j][i] = fmaf(f, red_o[x][4 * j + i][lane], o[j][i]);
+      }
+      top = all;
+    }
+  };
+  // lane (m, q) has the elements (D/16) (4q + i) + j of head m: D/16 in a row for every i
+  auto finish = [&](long long hd) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;             // (no weight at all: 0; NaN stays)
+    const long long to = hd * D + (D / 4) * q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < D / 16; j += 4) {
+        const float r[4] = {o[j][i] * inv, o[j + 1][i] * inv, o[j + 2][i] * inv, o[j + 3][i] * inv};
+        store_out<CACHE>(a.out, to + (D / 16) * i + j, r);
+      }
+    if (a.lse && q == 0) a.lse[hd] = ((top == -INFINITY ? 0.f : top) + log2f(sum)) * (1.f / kLog2e);
+  };
+  auto clear = [&]() {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    top = -INFINITY;
+    sum = 0.f;
+  };
+
+  while (u < u_end) {
+    locate(u);
     const int n_units = min(units - start, u_end - u);
     const int kv = udiv(row, blocks), g0 = (row - kv * blocks) * 16;
     const bool there = g0 + m < a.group;
@@ -307,10 +395,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
     const int32_t* table = a.block_table + (long long)b * a.max_pages;
     uint32_t qw[Tile::kQWords];
     load_query<CACHE, D>(qw, a, b * a.q_stride + (long long)head * D, there, q);
-    f32x4 o[D / 16];
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float top = -INFINITY, sum = 0.f;
+    clear();
 
     // this wave's tiles: kUnit apart from p0 on, those in front of p_end
     const int p0 = start * kUnit + w * kTile, p_end = min(len, (start + n_units) * kUnit);
@@ -391,123 +476,89 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-
-    // join of the waves, in their order
     if (bad) sum = NAN;
-    if (w > 0) {
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) red_o[w - 1][4 * j + i][lane] = o[j][i];
-      red_ml[w - 1][0][lane] = top;
-      red_ml[w - 1][1][lane] = sum;
-    }
-    __syncthreads();
-    const bool whole = n_units == units;
-    const int slot = 2 * blockIdx.x + (start == 0);
-    if (w == 0) {
-      float all = top;
-#pragma unroll
-      for (int x = 0; x < kAttWaves - 1; ++x) all = fmaxf(all, red_ml[x][0][lane]);
-      const float ref = all == -INFINITY ? 0.f : all;
-      float f = __builtin_amdgcn_exp2f(top - ref);
-      sum *= f;
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) o[j] *= f;
-#pragma unroll
-      for (int x = 0; x < kAttWaves - 1; ++x) {
-        f = __builtin_amdgcn_exp2f(red_ml[x][0][lane] - ref);
-        sum = fmaf(f, red_ml[x][1][lane], sum);
+
+    join_waves();
+    if (n_units == units) {
+      if (w == 0 && there) finish((long long)b * a.n_heads + head);
+    } else {
+      // A part: pairs of elements, lane after lane (elements of one head after the other would be written 8 bytes here and there:
+      // 40 us for 29 sequences of 1000 positions and 256 heads where this took 31)
+      const int r0 = first + row * units;
+      const Part mine_of = {b, row, cut.first_of(r0), cut.last_of(r0, units) - cut.first_of(r0) + 1};
+      part[n_parts > 0] = mine_of;
+      ++n_parts;
+      if (w == 0 && there) {
+        const int slot = 2 * blockIdx.x + (start == 0);
+        float2* to = a.part_o + (long long)slot * (D / 8) * pitch + mine_at;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[j][i] = fmaf(f, red_o[x][4 * j + i][lane], o[j][i]);
-      }
-      // element (D/16) (4q + i) + j: D/16 in a row for every i
-      if (there) {
-        if (whole) {
-          const float inv = inverse(sum);
-          const long long to = ((long long)b * a.n_heads + head) * D + (D / 4) * q;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < D / 16; j += 4) {
-              const float r[4] = {o[j][i] * inv, o[j + 1][i] * inv, o[j + 2][i] * inv, o[j + 3][i] * inv};
-              store_out<CACHE>(a.out, to + (D / 16) * i + j, r);
-            }
-          if (q == 0) finish_row<CACHE>(a, (long long)b * a.n_heads + head, ref, sum);
-        } else {
-          float* to = a.part_o + ((long long)slot * gmax + m) * D + (D / 4) * q;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < D / 16; j += 4)
-              store_through(to + (D / 16) * i + j, make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]));
-          if (q == 0) store_through(a.part_ml + (long long)slot * gmax + m, make_float2(all, sum));
-        }
-      }
-      if (!whole) {
-        // the row's parts are complete where the last one is counted
-        const int r0 = first + row * units, parts = udiv(r0 + units - 1, per) - udiv(r0, per) + 1;
-        // (until then the result is NaN: if the counters were not 0 at the start, nothing can pass for a result)
-        if (there && start == 0) {
+          for (int i = 0; i < 4; i += 2) store_through(to + (2 * j + i / 2) * pitch, make_float2(o[j][i], o[j][i + 1]));
+        if (q == 0) store_through(a.part_ml + (long long)slot * gmax + m, make_float2(top, sum));
+        // until the parts are joined the result is NaN: if the counters were not 0 at the start, nothing can pass for one
+        if (start == 0) {
           const float nan = __uint_as_float(0x7fc07fc0u);          // also as two bf16 numbers
-          unsigned char* to = static_cast<unsigned char*>(a.out) + (((long long)b * a.n_heads + head) * D + (D / 4) * q) * kOutBytes;
+          unsigned char* out = static_cast<unsigned char*>(a.out) + (((long long)b * a.n_heads + head) * D + (D / 4) * q) * kOutBytes;
 #pragma unroll
-          for (int i = 0; i < D / 4 * kOutBytes; i += 16)
-            store_through(reinterpret_cast<float*>(to + i), make_float4(nan, nan, nan, nan));
+          for (int i = 0; i < D / 4 * kOutBytes; i += 8) store_through(reinterpret_cast<float2*>(out + i), make_float2(nan, nan));
           if (a.lse && q == 0) store_through(a.lse + (long long)b * a.n_heads + head, nan);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (lane == 0) {
-          int32_t* const done = a.done + (long long)b * rows + row;
-          const int old = __hip_atomic_fetch_add(done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          if (old == parts - 1) __hip_atomic_store(done, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          last = old == parts - 1;
-        }
       }
     }
-    __syncthreads();
-    if (!whole && last) {
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-      // parts in the order of their workgroups: the first is that workgroup's second slot, the others their first.  Threads take
-      // four elements of a head each, as many threads as there are left share its parts.
-      const int r0 = first + row * units, w0 = udiv(r0, per), parts = udiv(r0 + units - 1, per) - w0 + 1;
-      const int heads = min(16, a.group - g0);
-      auto slot_of = [&](int p) { return 2 * (w0 + p) + (p == 0); };
-      for (int h = w; h < heads; h += kAttWaves) {             // a wave per head: 64 lanes = D/4 elements x 64 / (D/4) shares of the parts
-        constexpr int kLanes = D / 4, kShares = 64 / kLanes;
-        const int e = lane % kLanes * 4, share = lane / kLanes;
-        float all = -INFINITY;
-        for (int p = lane; p < parts; p += 64) all = fmaxf(all, a.part_ml[(long long)slot_of(p) * gmax + h].x);
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) all = fmaxf(all, __shfl_xor(all, off, 64));
-        const float ref = all == -INFINITY ? 0.f : all;
-        float l = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int p = share; p < parts; p += kShares) {
-          const long long sl = (long long)slot_of(p) * gmax + h;
-          const float2 ml = a.part_ml[sl];
-          const float4 v = *reinterpret_cast<const float4*>(a.part_o + sl * D + e);
-          const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-          l = fmaf(f, ml.y, l);
-          r[0] = fmaf(f, v.x, r[0]); r[1] = fmaf(f, v.y, r[1]); r[2] = fmaf(f, v.z, r[2]); r[3] = fmaf(f, v.w, r[3]);
-        }
-#pragma unroll
-        for (int off = kLanes; off < 64; off <<= 1) {
-          l += __shfl_xor(l, off, 64);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) r[i] += __shfl_xor(r[i], off, 64);
-        }
-        const float inv = inverse(l);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] *= inv;
-        const long long hd = (long long)b * a.n_heads + kv * a.group + g0 + h;
-        if (share == 0) store_out<CACHE>(a.out, hd * D + e, r);
-        if (lane == 0) finish_row<CACHE>(a, hd, ref, l);
-      }
-    }
+    __syncthreads();                        // red_o and red_ml have been read
     u += n_units;
+  }
+  if (n_parts == 0) return;
+
+  // A row's parts are complete where the last one is counted; that workgroup joins them.  (Counted at the end, when the first part's
+  // stores have long arrived.)
+  if (w == 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (lane < n_parts) {
+      const Part p = lane == 0 ? part[0] : part[1];
+      int32_t* const done = a.done + (long long)p.b * rows + p.row;
+      const int old = __hip_atomic_fetch_add(done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (old == p.parts - 1) __hip_atomic_store(done, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last[lane] = old == p.parts - 1;
+    }
+  }
+  __syncthreads();
+  for (int k = 0; k < n_parts; ++k) {
+    if (!last[k]) continue;
+    const Part pt = k == 0 ? part[0] : part[1];
+    const int kv = udiv(pt.row, blocks), g0 = (pt.row - kv * blocks) * 16;
+    const bool there = g0 + m < a.group;
+    // in the order of their workgroups, a fourth for each wave: the first is its workgroup's second slot, the others their first
+    clear();
+    const int p_begin = pt.parts * w / kAttWaves, p_last = pt.parts * (w + 1) / kAttWaves;
+#pragma unroll 2
+    for (int p = p_begin; p < p_last; ++p) {
+      const long long slot = 2 * (pt.first + p) + (p == 0);
+      float2 ml = make_float2(-INFINITY, 0.f), v[D / 8];
+#pragma unroll
+      for (int x = 0; x < D / 8; ++x) v[x] = make_float2(0.f, 0.f);
+      if (there) {
+        ml = load_through(a.part_ml + slot * gmax + m);
+        const float2* from = a.part_o + slot * (D / 8) * pitch + mine_at;
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x) v[x] = load_through(from + x * pitch);
+      }
+      const float next = fmaxf(top, ml.x), ref = next == -INFINITY ? 0.f : next;
+      const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(ml.x - ref);
+      top = next;
+      sum = sum * f + ml.y * g;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          o[j][i] = o[j][i] * f + v[2 * j + i / 2].x * g;
+          o[j][i + 1] = o[j][i + 1] * f + v[2 * j + i / 2].y * g;
+        }
+    }
+    join_waves();
+    if (w == 0 && there) finish((long long)pt.b * a.n_heads + kv * a.group + g0 + m);
+    __syncthreads();
   }
 }
 
@@ -554,8 +605,8 @@ hipError_t launch_cache_attention(const mohge_cache_config& c, const void* q, lo
   a.page_shift = log2_of(c.page_size); a.n_pages = c.n_pages; a.max_pages = c.max_pages;
   const int groups = att_groups(c), gmax = a.group < 16 ? a.group : 16;
   a.done = static_cast<int32_t*>(ws);
-  a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + att_done_bytes(c));
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)groups * 2 * gmax * c.head_size);
+  a.part_o = reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) + att_done_bytes(c));
+  a.part_ml = a.part_o + (size_t)groups * gmax * c.head_size;
   if (c.cache_dtype == MOHGE_F32) go_attention<kCacheF32>(a, c.head_size, groups, s);
   else if (c.cache_dtype == MOHGE_BF16) go_attention<kCacheBf16>(a, c.head_size, groups, s);
   else go_attention<kCacheE4m3>(a, c.head_size, groups, s);
