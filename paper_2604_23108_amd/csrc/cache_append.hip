@@ -1,22 +1,43 @@
 // New keys and values into the pages of a cache, for gfx950.  Bound by memory: every thread takes 8 elements of one
-// (token, head) row; with an E4M3 cache the threads of a row fold its largest magnitude before they convert.
+// (token, head) row of the keys and of the values, requests them, and looks up where they go meanwhile (a chain of loads: the token's
+// sequence, its length, its page); with an E4M3 cache the threads of a row fold its largest magnitude before they convert.
 #include "block.h"
 
 namespace mohge {
 
-// CACHE: type of the pages.  head_size / 8 threads (8, 16 or 32) share a row; blockIdx.y: 0 = keys, 1 = values.
+// 8 elements of a row to the pages: as they are, or as codes with a scale for the per_row threads (8, 16 or 32) of the row
+template <bool BF16, bool E4M3>
+__device__ __forceinline__ void store_piece(const Piece<BF16>& a, void* pages, float* scales, long long at, int per_row, int piece) {
+  if constexpr (E4M3) {
+    float x[8], top = 0.f;
+    a.get(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
+    for (int off = per_row >> 1; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    const float scale = e4m3_scale(top), inv = 1.f / scale;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= inv;
+    static_cast<uint2*>(pages)[at * per_row + piece] = to_e4m3x8(x);
+    if (piece == 0) scales[at] = scale;
+  } else {
+    a.store(pages, at * per_row + piece);
+  }
+}
+
 template <bool BF16, bool E4M3>
 __global__ void __launch_bounds__(256) cache_append_kernel(
     const mohge_cache_config c, const int n_tokens, const void* __restrict__ k, const long long k_stride,
     const void* __restrict__ v, const long long v_stride, const int32_t* __restrict__ tok_offsets,
     const int32_t* __restrict__ block_table, const int32_t* __restrict__ seq_lens, void* k_pages, void* v_pages,
     float* k_scale, float* v_scale, const int page_shift) {
-  const bool values = blockIdx.y != 0;
   const int per_row = c.head_size / 8, per_token = c.n_kv_heads * per_row;
   const unsigned idx = blockIdx.x * 256u + threadIdx.x;          // (fewer than 2^31 pieces)
   const int t = (int)(idx / (unsigned)per_token), rest = (int)(idx % (unsigned)per_token);
   if (t >= n_tokens) return;                       // whole rows: per_row divides the wave
   const int head = rest / per_row, piece = rest % per_row;
+  Piece<BF16> ka, va;
+  ka.load(k, t * k_stride / 8 + rest);
+  va.load(v, t * v_stride / 8 + rest);
   // the sequence: the last one whose first row is not behind this one
   int b = t, after = 1;
   if (tok_offsets) {
@@ -35,23 +56,8 @@ __global__ void __launch_bounds__(256) cache_append_kernel(
   const int page = block_table[(long long)b * c.max_pages + col];
   if ((unsigned)page >= (unsigned)c.n_pages) return;
   const long long at = (((long long)page * c.n_kv_heads + head) << page_shift) + (pos & (c.page_size - 1));
-  Piece<BF16> a;
-  a.load(values ? v : k, ((long long)t * (values ? v_stride : k_stride)) / 8 + rest);
-  void* const pages = values ? v_pages : k_pages;
-  if constexpr (E4M3) {
-    float x[8], top = 0.f;
-    a.get(x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
-    for (int off = per_row >> 1; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    const float scale = e4m3_scale(top), inv = 1.f / scale;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= inv;
-    static_cast<uint2*>(pages)[at * per_row + piece] = to_e4m3x8(x);
-    if (piece == 0) (values ? v_scale : k_scale)[at] = scale;
-  } else {
-    a.store(pages, at * per_row + piece);
-  }
+  store_piece<BF16, E4M3>(ka, k_pages, k_scale, at, per_row, piece);
+  store_piece<BF16, E4M3>(va, v_pages, v_scale, at, per_row, piece);
 }
 
 hipError_t launch_cache_append(const mohge_cache_config& c, int n_tokens, const void* k, long long k_stride,
@@ -59,7 +65,7 @@ hipError_t launch_cache_append(const mohge_cache_config& c, int n_tokens, const 
                                const int32_t* block_table, const int32_t* seq_lens, void* k_pages, void* v_pages,
                                float* k_scale, float* v_scale, hipStream_t s) {
   const long long threads = (long long)n_tokens * c.n_kv_heads * (c.head_size / 8);
-  const dim3 grid((unsigned)((threads + 255) / 256), 2);
+  const dim3 grid((unsigned)((threads + 255) / 256));
   auto go = [&](auto kern) {
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, c, n_tokens, k, k_stride, v, v_stride, tok_offsets, block_table,
                        seq_lens, k_pages, v_pages, k_scale, v_scale, log2_of(c.page_size));
