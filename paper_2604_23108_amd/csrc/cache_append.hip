@@ -1,6 +1,9 @@
-// New keys and values into the pages of a cache, for gfx950.  Bound by memory: every thread takes 8 elements of one
-// (token, head) row of the keys and of the values, requests them, and looks up where they go meanwhile (a chain of loads: the token's
-// sequence, its length, its page); with an E4M3 cache the threads of a row fold its largest magnitude before they convert.
+// New keys and values into the pages of a cache, for gfx950: token i of the n new ones of a sequence of (now) len positions goes to
+// position len - n + i, with an E4M3 cache as codes of x / scale, scale = max |x| / 448 over the token's row of one head.
+// Bound by memory: every thread takes 8 elements of one (token, head) row of the keys and of the values, requests them, and looks up
+// where they go meanwhile (a chain of loads: the token's sequence, its length, its page); with an E4M3 cache the threads of a row
+// fold its largest magnitude before they convert.  9003 tokens of 8 heads of 128 to 8 bits 13.5 us, 4.2 TB/s; 5023 of 4 heads of
+// 256 as they are 8.5 us, 4.8 TB/s; one token for each of 32 sequences 2.1 us, a launch.
 #include "block.h"
 
 namespace mohge {
@@ -24,20 +27,10 @@ __device__ __forceinline__ void store_piece(const Piece<BF16>& a, void* pages, f
   }
 }
 
-template <bool BF16, bool E4M3>
-__global__ void __launch_bounds__(256) cache_append_kernel(
-    const mohge_cache_config c, const int n_tokens, const void* __restrict__ k, const long long k_stride,
-    const void* __restrict__ v, const long long v_stride, const int32_t* __restrict__ tok_offsets,
-    const int32_t* __restrict__ block_table, const int32_t* __restrict__ seq_lens, void* k_pages, void* v_pages,
-    float* k_scale, float* v_scale, const int page_shift) {
-  const int per_row = c.head_size / 8, per_token = c.n_kv_heads * per_row;
-  const unsigned idx = blockIdx.x * 256u + threadIdx.x;          // (fewer than 2^31 pieces)
-  const int t = (int)(idx / (unsigned)per_token), rest = (int)(idx % (unsigned)per_token);
-  if (t >= n_tokens) return;                       // whole rows: per_row divides the wave
-  const int head = rest / per_row, piece = rest % per_row;
-  Piece<BF16> ka, va;
-  ka.load(k, t * k_stride / 8 + rest);
-  va.load(v, t * v_stride / 8 + rest);
+// Where token t goes: the row of the page array of its first head, negative if nowhere
+__device__ __forceinline__ long long token_place(const mohge_cache_config& c, const int t, const int32_t* __restrict__ tok_offsets,
+                                                 const int32_t* __restrict__ block_table, const int32_t* __restrict__ seq_lens,
+                                                 const int page_shift) {
   // the sequence: the last one whose first row is not behind this one
   int b = t, after = 1;
   if (tok_offsets) {
@@ -52,10 +45,32 @@ __global__ void __launch_bounds__(256) cache_append_kernel(
   }
   const int pos = seq_lens[b] - after;
   const int col = pos >> page_shift;
-  if (after < 1 || pos < 0 || col >= c.max_pages) return;
+  if (after < 1 || pos < 0 || col >= c.max_pages) return -1;
   const int page = block_table[(long long)b * c.max_pages + col];
-  if ((unsigned)page >= (unsigned)c.n_pages) return;
-  const long long at = (((long long)page * c.n_kv_heads + head) << page_shift) + (pos & (c.page_size - 1));
+  if ((unsigned)page >= (unsigned)c.n_pages) return -1;
+  return (((long long)page * c.n_kv_heads) << page_shift) + (pos & (c.page_size - 1));
+}
+
+template <bool BF16, bool E4M3>
+__global__ void __launch_bounds__(256) cache_append_kernel(
+    const mohge_cache_config c, const int n_tokens, const void* __restrict__ k, const long long k_stride,
+    const void* __restrict__ v, const long long v_stride, const int32_t* __restrict__ tok_offsets,
+    const int32_t* __restrict__ block_table, const int32_t* __restrict__ seq_lens, void* k_pages, void* v_pages,
+    float* k_scale, float* v_scale, const int page_shift) {
+  const int per_row = c.head_size / 8, per_token = c.n_kv_heads * per_row;
+  const unsigned idx = blockIdx.x * 256u + threadIdx.x;          // (fewer than 2^31 pieces)
+  const int t = (int)(idx / (unsigned)per_token), rest = (int)(idx % (unsigned)per_token);
+  if (t >= n_tokens) return;                       // whole rows: per_row divides the wave
+  const int head = rest / per_row, piece = rest % per_row;
+  Piece<BF16> ka, va;
+  ka.load(k, t * k_stride / 8 + rest);
+  va.load(v, t * v_stride / 8 + rest);
+  // a wave with one token looks it up with scalar loads (9003 tokens to 8 bits 15.9 us without, 13.5 with)
+  const int t0 = __builtin_amdgcn_readfirstlane(t);
+  long long at = __ballot(t != t0) == 0 ? token_place(c, t0, tok_offsets, block_table, seq_lens, page_shift)
+                                        : token_place(c, t, tok_offsets, block_table, seq_lens, page_shift);
+  if (at < 0) return;
+  at += (long long)head << page_shift;
   store_piece<BF16, E4M3>(ka, k_pages, k_scale, at, per_row, piece);
   store_piece<BF16, E4M3>(va, v_pages, v_scale, at, per_row, piece);
 }
