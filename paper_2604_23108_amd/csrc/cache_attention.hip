@@ -16,11 +16,17 @@
 // product and keeps them as good as fp32: one bf16 rounding of them would be as large as the output's own.
 // fp32 caches go through the fp32 matrix cores (16x16x4) with the same assignment, four positions at a time.
 //
-// Work split: the positions of every (sequence, kv head, block of 16 query heads) are cut into units of 128, one tile of 32 for each
-// wave, and the units of all of them, in one row, into equal stretches, one for each workgroup: whatever the lengths, every
-// workgroup has the same number of units.  The stretches follow from the lengths, which every workgroup reads for itself.
-// A row that lies in several stretches leaves parts (sums, maximum and total) in the workspace, and the workgroup that finishes last
-// joins them in their order.
+// Work split: the positions of every (sequence, kv head, block of 16 query heads) are cut into units of four tiles, one for each wave (128
+// positions, or 64 where a tile is one half), and the units of all of them, in one row, into equal stretches, one for each workgroup that
+// the machine holds at once: whatever the lengths, every workgroup has about the same number of units.  The stretches follow from
+// the lengths, which every workgroup reads for itself.  A row that lies in several stretches leaves parts (sums, maximum and total)
+// in the workspace, and the workgroup that finishes last joins them in their order: how many parts there are depends on the
+// lengths alone, so equal calls have equal results.
+//
+// Measured (us; TB/s of keys and values; bf16, 32 query heads over 8 kv heads of 128, pages of 16): 32 sequences of 4096 97..100, 5.4;
+// 32 of 0..8191 112, 4.8; two of some 115000, 8 bits, 104, 4.7; one of 1531 (16 over 4 heads of 64) 7.4.  The loads alone, without any
+// arithmetic on what they bring, take as long (99.7, 116 for 117, 7.5): the kernel is bound by its reads, and short calls by a launch and a
+// chain of five dependent accesses (length, page, tile, part and counter, parts).
 #include "block.h"
 
 namespace mohge {
@@ -58,10 +64,13 @@ __device__ __forceinline__ uint32_t cvt_bf16x2(uint32_t codes, bool hi) {
   return __builtin_bit_cast(uint32_t, r);
 }
 
+typedef short bf16x4 __attribute__((ext_vector_type(4)));
+
 union AttFrag {
   uint4 u;
   uint32_t w[4];
   bf16x8 v;
+  bf16x4 half;
 };
 
 // N bytes (4, 8 or multiples of 16) at p into words
@@ -80,10 +89,16 @@ __device__ __forceinline__ void load_bytes(uint32_t* w, const unsigned char* p) 
   }
 }
 
+// Halves of 16 positions in a tile.  One where two would leave the registers to a single wave per SIMD (us with two and with one, 32
+// query heads over 8 kv heads): E4M3 of 256, 128 sequences of up to 300 positions 47.5 and 35.1, 32 of up to 4096 76 and 67, 32 of
+// 4096 105 and 106; fp32 of 128, the same 60 and 47, 113 and 109, 190 and 194.  A bf16 cache of 256 stays with two: 58 and 54, 114 and 122.
+constexpr int att_halves(int cache, int d) {
+  return cache == kCacheF32 ? (d == 64 ? 2 : 1) : cache == kCacheE4m3 && d == 256 ? 1 : 2;
+}
+
 template <int CACHE, int D>
 struct AttTile {
-  // halves of 16 positions: two, but for the widest rows, whose second half would not fit the registers
-  static constexpr int H = CACHE == kCacheF32 && D == 256 ? 1 : 2;
+  static constexpr int H = att_halves(CACHE, D);
   static constexpr int kBytes = CACHE == kCacheF32 ? 4 : CACHE == kCacheBf16 ? 2 : 1;
   static constexpr int kRow = D * kBytes;
   static constexpr int kKeyLoads = kRow / 64;             // 16 bytes per lane each, 64 bytes of a key's row
@@ -150,6 +165,12 @@ struct AttTile {
     if constexpr (CACHE == kCacheE4m3) vs[hf][i] = 0.f;
   }
 
+  // V^T p over the positions of the halves (4 or 8 per lane)
+  static __device__ __forceinline__ f32x4 product(const AttFrag& v, const AttFrag& p, const f32x4 o) {
+    if constexpr (H == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p.v, o, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v.half, p.half, o, 0, 0, 0);
+  }
+
   // o += V^T p for all halves
   __device__ __forceinline__ void values(f32x4 (&o)[D / 16], const float (&p)[H][4]) const {
     if constexpr (CACHE == kCacheF32) {
@@ -163,7 +184,7 @@ struct AttTile {
     } else {
       AttFrag hi, lo;
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
+      for (int hf = 0; hf < H; ++hf)
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
           float a = p[hf][i], b = p[hf][i + 1];
@@ -176,7 +197,7 @@ struct AttTile {
       for (int jj = 0; jj < D / 32; ++jj) {                  // elements 2jj and 2jj + 1
         AttFrag f0, f1;
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
+        for (int hf = 0; hf < H; ++hf) {
           uint32_t r[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -189,10 +210,10 @@ struct AttTile {
             f1.w[2 * hf + i / 2] = __builtin_amdgcn_perm(r[i + 1], r[i], 0x07060302u);
           }
         }
-        o[2 * jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0.v, hi.v, o[2 * jj], 0, 0, 0);
-        o[2 * jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0.v, lo.v, o[2 * jj], 0, 0, 0);
-        o[2 * jj + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1.v, hi.v, o[2 * jj + 1], 0, 0, 0);
-        o[2 * jj + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1.v, lo.v, o[2 * jj + 1], 0, 0, 0);
+        o[2 * jj] = product(f0, hi, o[2 * jj]);
+        o[2 * jj] = product(f0, lo, o[2 * jj]);
+        o[2 * jj + 1] = product(f1, hi, o[2 * jj + 1]);
+        o[2 * jj + 1] = product(f1, lo, o[2 * jj + 1]);
       }
     }
   }
@@ -254,11 +275,10 @@ __device__ __forceinline__ void store_through(float* p, const float v) {
 // Stretches of `per` units begin at multiples of it, except in rows that are short or hardly longer than a stretch: those are not cut, a
 // stretch begins at their nearer end.  (A part has to be written, counted and read again: 464 rows of 8 units in stretches
 // of 5 take 20.8 us cut and 17.6 whole, 32 rows of 4 units 12.0 and 9.5.)
-template <int SHORT>
 struct Stretches {
   int per;
   __device__ __forceinline__ bool keep_whole(int units) const {
-    return units <= SHORT || (units >= per && units <= per + max(1, per / 2));
+    return units <= 4 || (units >= per && units <= per + max(1, per / 2));
   }
   // unit v, which is unit `start` of a row of `units`
   __device__ __forceinline__ int begin(int v, int start, int units) const {
@@ -294,9 +314,9 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
   for (int b0 = 64; b0 < a.n_seqs; b0 += 64)
     total += __builtin_amdgcn_readlane(wave_incl_scan(b0 + lane < a.n_seqs ? units_of<kUnit>(a, b0 + lane) : 0), 63);
   total *= rows;
-  // (two units at least where rows are long: with one, more parts are joined than it helps)
-  Stretches<CACHE == kCacheF32 ? 1 : 4> cut;          // (an fp32 unit takes as long as a part costs)
-  cut.per = max(udiv(total + (int)gridDim.x - 1, gridDim.x), total >= 8ll * a.n_seqs * rows ? 2 : 1);
+  // (two units at least where rows have 1024 positions in the mean: with one, more parts are joined than it helps)
+  Stretches cut;
+  cut.per = max(udiv(total + (int)gridDim.x - 1, gridDim.x), total >= 1024ll / kUnit * a.n_seqs * rows ? 2 : 1);
   int before = 0;                                 // units (of one row) in front of sequence `base`
   // the sequence b of unit v (at least as far as the last one asked for), its row, the unit's place in the row
   int b, units, first, row, start;
@@ -564,7 +584,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
 
 // Waves per SIMD that the registers of a form allow (two tiles and the sums of one)
 constexpr int att_waves(int cache, int d) {
-  return cache == kCacheF32 ? (d == 64 ? 2 : 1) : cache == kCacheBf16 ? (d == 64 ? 3 : d == 128 ? 2 : 1) : d == 64 ? 3 : d == 128 ? 2 : 1;
+  return d == 256 ? (cache == kCacheE4m3 ? 2 : 1) : d == 64 && cache != kCacheF32 ? 3 : 2;
 }
 
 static int att_rows(const mohge_cache_config& c) { return c.n_kv_heads * ((c.n_heads / c.n_kv_heads + 15) / 16); }
@@ -572,7 +592,7 @@ static int att_rows(const mohge_cache_config& c) { return c.n_kv_heads * ((c.n_h
 // Workgroups: as many as are resident at once, no more than there can be units
 static int att_groups(const mohge_cache_config& c) {
   const int cache = c.cache_dtype == MOHGE_F32 ? kCacheF32 : c.cache_dtype == MOHGE_BF16 ? kCacheBf16 : kCacheE4m3;
-  const int unit = (cache == kCacheF32 && c.head_size == 256 ? 16 : 32) * kAttWaves;
+  const int unit = 16 * att_halves(cache, c.head_size) * kAttWaves;
   const long long units = (long long)c.n_seqs * att_rows(c) * (((long long)c.max_pages * c.page_size + unit - 1) / unit);
   const long long most = 256 * att_waves(cache, c.head_size);
   return (int)(units < most ? units : most);
