@@ -72,7 +72,7 @@ typedef struct mohge_cache_config {
   int32_t head_size;    /* 64, 128 or 256                                                          */
   int32_t page_size;    /* 16, 32, 64, 128 or 256                                                  */
   int32_t n_pages;
-  int32_t max_pages;    /* columns of block_table; max_pages * page_size < 2^31                    */
+  int32_t max_pages;    /* columns of block_table; max_pages * page_size <= 2^30                   */
   int32_t dtype;        /* MOHGE_F32 or MOHGE_BF16: q, k, v, out                                   */
   int32_t cache_dtype;  /* dtype, or MOHGE_E4M3 with MOHGE_BF16                                    */
 } mohge_cache_config;

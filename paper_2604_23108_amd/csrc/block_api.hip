@@ -34,8 +34,9 @@ int check_cache(const mohge_cache_config* c) {
   if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) {
     set_error("page_size = %d must be 16, 32, 64, 128 or 256", c->page_size); return MOHGE_EINVAL; }
   if (c->n_pages < 1 || c->max_pages < 1) { set_error("n_pages and max_pages must be positive"); return MOHGE_EINVAL; }
-  if ((int64_t)c->max_pages * c->page_size >= (int64_t)1 << 31) {
-    set_error("max_pages*page_size does not fit int32"); return MOHGE_EINVAL; }
+  // (positions are int32, and the attention rounds them up to its units)
+  if ((int64_t)c->max_pages * c->page_size > (int64_t)1 << 30) {
+    set_error("max_pages*page_size must be at most 2^30: positions are int32"); return MOHGE_EINVAL; }
   // (the attention numbers its units of 64 positions or more in 32 bits)
   if ((int64_t)c->n_seqs * c->n_heads * ((int64_t)c->max_pages * c->page_size / 64 + 1) >= (int64_t)1 << 31) {
     set_error("n_seqs*n_heads*max_pages*page_size must be less than 2^37"); return MOHGE_EINVAL; }

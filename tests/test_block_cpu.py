@@ -197,3 +197,12 @@ def test_pages_are_handed_out_and_taken_back():
     assert kv.seq_lens.tolist() == [0, 1, 17] and kv.block_table[0].tolist() == [-1] * 4
     kv.grow([64, 0, 0])
     assert len(kv.pages[0]) == 4 and len({p for pages in kv.pages for p in pages}) == 7
+
+
+def test_positions_leave_room_for_rounding_up():
+    """Lengths are rounded up to a unit of the attention in int32: a table for 2^31 - 16 positions would overflow there."""
+    one = dict(n_seqs=1, n_heads=1, n_kv_heads=1, head_size=64, page_size=16, n_pages=10)
+    assert M.mohge_cache_workspace_size(M.CacheConfig(**one, max_pages=1 << 26)) > 0
+    for pages in ((1 << 26) + 1, (1 << 27) - 1):
+        assert M.mohge_cache_workspace_size(M.CacheConfig(**one, max_pages=pages)) == 0
+        assert "int32" in M.mohge_last_error()
