@@ -24,7 +24,7 @@
 // lengths alone, so equal calls have equal results.
 //
 // Measured (us; TB/s of keys and values; bf16, 32 query heads over 8 kv heads of 128, pages of 16): 32 sequences of 4096 97..100, 5.4;
-// 32 of 0..8191 112, 4.8; two of some 115000, 8 bits, 104, 4.7; one of 1531 (16 over 4 heads of 64) 7.4.  The loads alone, without any
+// 32 of 0..8191 112, 4.8; two of some 115000, 8 bits, 104, 4.7; one of 1531 (16 over 4 heads of 64) 7.6.  The loads alone, without any
 // arithmetic on what they bring, take as long (99.7, 116 for 117, 7.5): the kernel is bound by its reads, and short calls by a launch and a
 // chain of five dependent accesses (length, page, tile, part and counter, parts).
 #include "block.h"
@@ -273,12 +273,13 @@ __device__ __forceinline__ void store_through(float* p, const float v) {
 }
 
 // Stretches of `per` units begin at multiples of it, except in rows that are short or hardly longer than a stretch: those are not cut, a
-// stretch begins at their nearer end.  (A part has to be written, counted and read again: 464 rows of 8 units in stretches
-// of 5 take 20.8 us cut and 17.6 whole, 32 rows of 4 units 12.0 and 9.5.)
+// stretch begins at their nearer end.  (A part has to be written, counted and read again: 464 rows of 8 units in stretches of 5 take
+// 20.8 us cut and 17.6 whole.  Short are 3 units, or 4 of an 8-bit cache: 128 rows of 4 units 13.3 us cut and 18.3 whole, 8 of 3 units
+// 8.4 and 7.5; 32 of 4 units in 8 bits 9.0 and 8.4.)
 struct Stretches {
-  int per;
+  int per, few;
   __device__ __forceinline__ bool keep_whole(int units) const {
-    return units <= 4 || (units >= per && units <= per + max(1, per / 2));
+    return units <= few || (units >= per && units <= per + max(1, per / 2));
   }
   // unit v, which is unit `start` of a row of `units`
   __device__ __forceinline__ int begin(int v, int start, int units) const {
@@ -316,6 +317,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
   total *= rows;
   // (two units at least where rows have 1024 positions in the mean: with one, more parts are joined than it helps)
   Stretches cut;
+  cut.few = CACHE == kCacheE4m3 ? 4 : 3;
   cut.per = max(udiv(total + (int)gridDim.x - 1, gridDim.x), total >= 1024ll / kUnit * a.n_seqs * rows ? 2 : 1);
   int before = 0;                                 // units (of one row) in front of sequence `base`
   // the sequence b of unit v (at least as far as the last one asked for), its row, the unit's place in the row
@@ -549,21 +551,10 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
     const Part pt = k == 0 ? part[0] : part[1];
     const int kv = udiv(pt.row, blocks), g0 = (pt.row - kv * blocks) * 16;
     const bool there = g0 + m < a.group;
-    // in the order of their workgroups, a fourth for each wave: the first is its workgroup's second slot, the others their first
+    // In the order of their workgroups, a fourth for each wave: the first is its workgroup's second slot, the others their first.
     clear();
     const int p_begin = pt.parts * w / kAttWaves, p_last = pt.parts * (w + 1) / kAttWaves;
-#pragma unroll 2
-    for (int p = p_begin; p < p_last; ++p) {
-      const long long slot = 2 * (pt.first + p) + (p == 0);
-      float2 ml = make_float2(-INFINITY, 0.f), v[D / 8];
-#pragma unroll
-      for (int x = 0; x < D / 8; ++x) v[x] = make_float2(0.f, 0.f);
-      if (there) {
-        ml = load_through(a.part_ml + slot * gmax + m);
-        const float2* from = a.part_o + slot * (D / 8) * pitch + mine_at;
-#pragma unroll
-        for (int x = 0; x < D / 8; ++x) v[x] = load_through(from + x * pitch);
-      }
+    auto add = [&](const float2 ml, const float2 (&v)[D / 8]) {
       const float next = fmaxf(top, ml.x), ref = next == -INFINITY ? 0.f : next;
       const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(ml.x - ref);
       top = next;
@@ -575,6 +566,49 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
           o[j][i] = o[j][i] * f + v[2 * j + i / 2].x * g;
           o[j][i + 1] = o[j][i + 1] * f + v[2 * j + i / 2].y * g;
         }
+    };
+    if (gmax > 8 || pt.parts <= 3 * kAttWaves) {
+#pragma unroll 2
+      for (int p = p_begin; p < p_last; ++p) {
+        const long long slot = 2 * (pt.first + p) + (p == 0);
+        float2 ml = make_float2(-INFINITY, 0.f), v[D / 8];
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x) v[x] = make_float2(0.f, 0.f);
+        if (there) {
+          ml = load_through(a.part_ml + slot * gmax + m);
+          const float2* from = a.part_o + slot * (D / 8) * pitch + mine_at;
+#pragma unroll
+          for (int x = 0; x < D / 8; ++x) v[x] = load_through(from + x * pitch);
+        }
+        add(ml, v);
+      }
+    } else {
+      // Many parts of up to 8 heads: the lanes that the heads leave over take parts as well, lane m has head m mod 2^lg and every (16 >> lg)th
+      // part of the wave (32 heads over 8: one sequence of 16000 positions, 63 parts a row, 28 us, 37 with the heads' lanes alone; one
+      // of 4000, 16 parts, 11.8 and 12.7; with fewer the exchange at the end takes longer than it saves).  A lane whose part or head is
+      // another lane's loads that and counts it with a weight of 0, or nowhere.
+      const int lg = gmax > 4 ? 3 : gmax > 2 ? 2 : gmax - 1;
+      const int hm = min(m & ((1 << lg) - 1), gmax - 1);
+#pragma unroll 2
+      for (int p0 = p_begin; p0 < p_last; p0 += 16 >> lg) {
+        const int p = min(p0 + (m >> lg), p_last - 1);
+        const long long slot = 2 * (pt.first + p) + (p == 0);
+        float2 ml = load_through(a.part_ml + slot * gmax + hm), v[D / 8];
+        const float2* from = a.part_o + slot * (D / 8) * pitch + q * gmax + hm;
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x) v[x] = load_through(from + x * pitch);
+        if (p0 + (m >> lg) >= p_last) ml = make_float2(-INFINITY, 0.f);
+        add(ml, v);
+      }
+      for (int off = 1 << lg; off < 16; off <<= 1) {
+        const float2 ml = make_float2(__shfl_xor(top, off, 64), __shfl_xor(sum, off, 64));
+        float2 v[D / 8];
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) v[2 * j + i / 2] = make_float2(__shfl_xor(o[j][i], off, 64), __shfl_xor(o[j][i + 1], off, 64));
+        add(ml, v);
+      }
     }
     join_waves();
     if (w == 0 && there) finish((long long)pt.b * a.n_heads + kv * a.group + g0 + m);

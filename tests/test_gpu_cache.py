@@ -328,3 +328,11 @@ def test_same_bits_every_time_on_any_stream_and_in_a_graph_whose_lengths_change(
         assert all(torch.equal(a, b) for a, b in zip(results(), eager)), i
     for b, n in enumerate(kv.lengths):
         assert kv.seq_lens[b] == n
+
+
+@pytest.mark.parametrize("group", [1, 2, 3, 5, 8, 16])
+@pytest.mark.parametrize("dtype,cache", KINDS)
+def test_many_parts_for_every_number_of_heads(group, dtype, cache):
+    """Rows that more than a dozen workgroups share, where heads leave lanes over for parts."""
+    cfg = M.CacheConfig(2, 2 * group, 2, 64, 16, 700, 600, dtype=dtype, cache_dtype=cache)
+    _attend(cfg, [9001, 77], 11)
