@@ -78,10 +78,9 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_kernel(
   }
   if (row >= T) return;
   const float rstd = rsqrtf(ss * inv_d + eps);
-  float scale = 1.f, inv_scale = 1.f;
+  float scale = 1.f;
   if constexpr (Q8) {
-    scale = e4m3_scale(top * rstd);
-    inv_scale = 1.f / scale;
+    scale = e4m3_scale(top * rstd);          // top * rstd is the largest |y| as it is rounded below: rounding keeps the order
     if (t == 0) y_scale[row] = scale;
   }
   if (rstd_out && t == 0) rstd_out[row] = rstd;
@@ -95,13 +94,14 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_kernel(
         o.store(sum_out, base + p);
       }
       float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = h[i][j] * rstd * w[i][j];
       if constexpr (Q8) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= inv_scale;
+        for (int j = 0; j < 8; ++j) v[j] = h[i][j] * w[i][j] * rstd;
+        divide_by_scale<2>(v, scale);
         static_cast<uint2*>(y)[base + p] = to_e4m3x8(v);
       } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = h[i][j] * rstd * w[i][j];
         o.set(v);
         o.store(y, base + p);
       }
