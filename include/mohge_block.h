@@ -105,7 +105,7 @@ int mohge_cache_append(const mohge_cache_config* cfg, int32_t n_tokens, const vo
  * workspace DEVICE, mohge_cache_workspace_size(cfg) bytes (a few MB, whatever the lengths; never less for more sequences).  It
  * holds counters that MUST BE ZERO when the call starts and that the call leaves zero: clear it once (hipMemset) and keep
  * it for calls of one cfg, issued in stream order; calls that overlap on one workspace race.  Were the counters not zero, results that
- * are joined from parts stay NaN.
+ * are joined from parts are NaN, in this call and in later ones, until the workspace is cleared.
  * The positions of all sequences are divided evenly over the workgroups, by the lengths found on the device; parts are
  * joined in a fixed order (deterministic).
  */

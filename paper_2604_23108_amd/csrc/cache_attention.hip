@@ -50,7 +50,7 @@ struct AttArgs {
   const float* v_scale;
   void* out;
   float* lse;
-  int32_t* done;              // [rows]: parts of a row that are complete; 0 between calls
+  unsigned long long* done;   // [rows]: parts of a row that are complete, in units of part_unit; 0 between calls
   float2* part_o;             // [2 per workgroup][D / 8][4][heads of a row]: pairs of a lane's elements, lane after lane
   float2* part_ml;            // [2 per workgroup][heads of a row]: maximum (of s log2 e) and sum
   float scale2;               // scale * log2 e
@@ -289,6 +289,14 @@ struct Stretches {
   __device__ __forceinline__ int first_of(int r0) const { return udiv(r0, per); }
   __device__ __forceinline__ int last_of(int r0, int units) const { return udiv(r0 + units - 1, per); }
 };
+
+// What a part adds to its row's counter.  Odd and far from every small number's multiple, another one for another number of parts: only a
+// counter that was 0 comes to parts * part_unit(parts), at the last part.  From any other start (numbers that the memory held, what calls
+// that overlapped left) it does not, in this call or a later one; counted by ones, a counter of 1 would have parts joined that are not
+// written yet, and be 1 again afterwards.  (2^64 over the golden ratio, and 2^64 (sqrt 2 - 1).)
+__device__ __forceinline__ unsigned long long part_unit(int parts) {
+  return 0x9e3779b97f4a7c15ull + (unsigned long long)parts * 0x6a09e667f3bcc909ull;
+}
 
 // A row of which this workgroup has a part
 struct Part {
@@ -539,10 +547,11 @@ __global__ void __launch_bounds__(64 * kAttWaves, OCC) cache_attention_kernel(co
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (lane < n_parts) {
       const Part p = lane == 0 ? part[0] : part[1];
-      int32_t* const done = a.done + (long long)p.b * rows + p.row;
-      const int old = __hip_atomic_fetch_add(done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (old == p.parts - 1) __hip_atomic_store(done, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last[lane] = old == p.parts - 1;
+      unsigned long long* const done = a.done + (long long)p.b * rows + p.row;
+      const unsigned long long unit = part_unit(p.parts), all = (unsigned long long)p.parts * unit;
+      const bool complete = __hip_atomic_fetch_add(done, unit, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + unit == all;
+      if (complete) __hip_atomic_fetch_add(done, 0ull - all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last[lane] = complete;
     }
   }
   __syncthreads();
@@ -632,7 +641,7 @@ static int att_groups(const mohge_cache_config& c) {
   return (int)(units < most ? units : most);
 }
 
-static size_t att_done_bytes(const mohge_cache_config& c) { return ((size_t)c.n_seqs * att_rows(c) * sizeof(int32_t) + 255) / 256 * 256; }
+static size_t att_done_bytes(const mohge_cache_config& c) { return ((size_t)c.n_seqs * att_rows(c) * sizeof(unsigned long long) + 255) / 256 * 256; }
 
 size_t cache_workspace_bytes(const mohge_cache_config& c) {
   const int group = c.n_heads / c.n_kv_heads, gmax = group < 16 ? group : 16;
@@ -658,7 +667,7 @@ hipError_t launch_cache_attention(const mohge_cache_config& c, const void* q, lo
   a.n_seqs = c.n_seqs; a.n_heads = c.n_heads; a.n_kv = c.n_kv_heads; a.group = c.n_heads / c.n_kv_heads;
   a.page_shift = log2_of(c.page_size); a.n_pages = c.n_pages; a.max_pages = c.max_pages;
   const int groups = att_groups(c), gmax = a.group < 16 ? a.group : 16;
-  a.done = static_cast<int32_t*>(ws);
+  a.done = static_cast<unsigned long long*>(ws);
   a.part_o = reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) + att_done_bytes(c));
   a.part_ml = a.part_o + (size_t)groups * gmax * c.head_size;
   if (c.cache_dtype == MOHGE_F32) go_attention<kCacheF32>(a, c.head_size, groups, s);
