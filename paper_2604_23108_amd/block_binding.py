@@ -185,7 +185,8 @@ class KVCache:
     """Pages of keys and values, which sequence has which, and how long each sequence is.
 
     The page numbers are handed out on the host: `grow` gives every sequence the pages that its new positions need and
-    sets the lengths, `append` writes their keys and values, `attend` reads.  `free` gives a sequence's pages back.
+    sets the lengths, `append` writes their keys and values, `attend` reads.  `free` gives a sequence's pages back.  The tensors
+    stay the same ones, so that recorded calls see what `grow` and `free` change.
     """
 
     def __init__(self, cfg: CacheConfig, device="cuda"):
@@ -195,7 +196,10 @@ class KVCache:
         scales = cfg.cache_dtype == E4M3
         self.k_scale, self.v_scale = (torch.ones(pages[:3], device=device) if scales else None for _ in range(2))
         self.block_table = torch.full((cfg.n_seqs, cfg.max_pages), -1, dtype=torch.int32, device=device)
-        self.seq_lens = torch.zeros(cfg.n_seqs, dtype=torch.int32, device=device)
+        # the lengths, and those of the sequences that the last `grow` made longer (0: the others); rows start 16 bytes apart
+        self._lens = torch.zeros((2, -(-cfg.n_seqs // 4) * 4), dtype=torch.int32, device=device)
+        self.seq_lens, self._grown = (row[:cfg.n_seqs] for row in self._lens)
+        self._all_grew = True
         self.out = torch.empty((cfg.n_seqs, cfg.n_heads, cfg.head_size), dtype=torch_type(cfg.dtype), device=device)
         self.lse = torch.empty((cfg.n_seqs, cfg.n_heads), dtype=torch.float32, device=device)
         self.ws = torch.zeros(max(16, mohge_cache_workspace_size(cfg)), dtype=torch.uint8, device=device)
@@ -225,23 +229,27 @@ class KVCache:
                     pages.append(self.pages[b][-1])
             at = torch.tensor([rows, cols, pages], device=self.block_table.device)
             self.block_table[at[0], at[1]] = at[2].int()
-        if len(set(new)) == 1:
-            self.seq_lens += new[0]
+        all_grew, had = all(n or not length for n, length in zip(new, lengths)), self._all_grew
+        self._all_grew = all_grew
+        if had and all_grew and len(set(new)) == 1:
+            self._lens += new[0]                           # the rows are equal and stay so
         else:
-            self.seq_lens += torch.tensor(list(new), dtype=torch.int32, device=self.seq_lens.device)
+            counts = torch.tensor(list(new), dtype=torch.int32, device=self._lens.device)
+            self.seq_lens += counts
+            self._grown.copy_(self.seq_lens * (counts > 0))
 
     def free(self, seq: int):
         """The sequence is empty again, its pages are handed out anew."""
         self._unused += reversed(self.pages[seq])
         self.pages[seq], self.lengths[seq] = [], 0
         self.block_table[seq] = -1
-        self.seq_lens[seq] = 0
+        self.seq_lens[seq] = self._grown[seq] = 0
 
     def append(self, k: torch.Tensor, v: torch.Tensor, tok_offsets: Optional[torch.Tensor] = None):
         """Keys and values of the positions that the last `grow` added: rows tok_offsets[b] .. of k and v for sequence b, or one
-        for every sequence."""
-        mohge_cache_append(self.cfg, k, v, tok_offsets, self.block_table, self.seq_lens, self.k_pages, self.v_pages,
-                           self.k_scale, self.v_scale)
+        row for every sequence, its last position; there the rows of sequences that did not grow are left out."""
+        lens = self._grown if tok_offsets is None else self.seq_lens
+        mohge_cache_append(self.cfg, k, v, tok_offsets, self.block_table, lens, self.k_pages, self.v_pages, self.k_scale, self.v_scale)
 
     def attend(self, q: torch.Tensor, scale: Optional[float] = None) -> torch.Tensor:
         """Attention of one query row per sequence over all its positions (scale: 1 / sqrt(head_size) unless given)."""
