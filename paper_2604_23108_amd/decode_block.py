@@ -9,7 +9,7 @@ caller's; several blocks are stacked by handing `forward`'s two results to the n
 from __future__ import annotations
 
 import argparse
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
@@ -41,10 +41,12 @@ class DecodeBlock:
         self.out = ProjW4(ProjConfig(T, self.q_size, d, group=group), *out)
         self.layer_norm = ResidualNorm(NormConfig(T, d, eps=eps), layer_norm)
 
-    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
-        """x [seqs, d]: the output of the block before (with the residual stream that came with it) or the embeddings."""
-        c = self.cache.cfg
-        self.cache.grow([1] * c.n_seqs)
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, active: Optional[Sequence[bool]] = None):
+        """x [seqs, d]: the output of the block before (with the residual stream that came with it) or the embeddings.
+        `active` says which sequences have a new token (all unless given).  The cache of the others stays as it is (a finished one's
+        pages are given back by `cache.free`); their rows of x hold any finite numbers, their rows of the results mean nothing."""
+        n = self.cache.cfg.n_seqs
+        self.cache.grow([1] * n if active is None else [int(bool(a)) for a in active])
         return self.step(x, residual)
 
     def step(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
