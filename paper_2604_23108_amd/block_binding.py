@@ -46,7 +46,8 @@ class _Native:
     """The extension module, loaded and given the library's entry points at the first call."""
 
     def __getattr__(self, name):
-        path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_block_native.so")
+        from .build import native_path
+        path = native_path(torch.__version__)
         if not os.path.exists(path):
             raise MohgeError(f"{path} is missing: build it with `python -m paper_2604_23108_amd.build` (there is no fallback path)")
         spec = importlib.util.spec_from_file_location("_block_native", path)
@@ -57,6 +58,7 @@ class _Native:
         module.bind(MohgeError, *[C.cast(getattr(lib(), e), C.c_void_p).value for e in entries])
         for n in ("rmsnorm", "rmsnorm_bwd", "cache_append", "cache_attention", "proj_w4"):
             setattr(self, n, getattr(module, n))
+        self.file = path
         return self.__dict__[name]
 
 

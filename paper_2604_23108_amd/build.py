@@ -1,6 +1,7 @@
 """Builds the shared libraries in-tree: with hipcc for gfx950 libmohge.so (the C-ABI library, include/mohge.h and
 mohge_block.h) and libmohge_bench.so (measurement and test aids, include/mohge_bench.h, linked against the first), with the
-host compiler _block_native.so (Python marshalling of mohge_block.h)."""
+host compiler the extension module _block_native (Python marshalling of mohge_block.h; the two libraries do without it and without
+torch)."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -19,7 +20,6 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libmohge.so")
 BENCH_LIB = os.path.join(HERE, "libmohge_bench.so")
-NATIVE = os.path.join(HERE, "_block_native.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["api.hip", "block_api.hip", "norm.hip", "cache_append.hip", "cache_attention.hip", "proj_w4.hip", "route.hip", "permute.hip", "ffn.hip", "ffn_f32.hip", "ffn_tiled.hip", "ffn_skinny.hip",
@@ -75,19 +75,31 @@ def _link(out: str, objs, extra=()) -> None:
         raise RuntimeError("link failed:\n" + p.stderr)
 
 
-def _native(_=None) -> None:
-    """The extension module: no device code.  torch's libraries are in the process before it is loaded (no run path)."""
-    import torch
+def native_path(torch_version: str) -> str:
+    """The extension module's file, named after the Python and the torch it is compiled for."""
+    return os.path.join(HERE, f"_block_native.{sysconfig.get_config_var('SOABI')}.torch{torch_version}.so")
+
+
+def _native() -> str:
+    """The extension module: no device code.  torch's libraries are in the process before it is loaded (no run path).  Returns its path,
+    or '' where there is no torch."""
+    try:
+        import torch
+    except ImportError:
+        sys.stderr.write("torch cannot be imported: the C libraries are built without the Python module\n")
+        return ""
+    out = native_path(torch.__version__)
     root, rocm = os.path.dirname(torch.__file__), os.environ.get("ROCM_PATH", "/opt/rocm")
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
            "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
            "-isystem", os.path.join(rocm, "include"), "-isystem", sysconfig.get_paths()["include"],
-           os.path.join(CSRC, "block_py.cpp"), "-o", NATIVE, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu",
+           os.path.join(CSRC, "block_py.cpp"), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu",
            "-lc10", "-lc10_hip"]
     p = subprocess.run(cmd, capture_output=True, text=True)
     if p.returncode != 0:
         raise RuntimeError(f"the host compiler failed for block_py.cpp:\n{p.stderr}")
+    return out
 
 
 def build(verbose: bool = False) -> str:
@@ -95,12 +107,12 @@ def build(verbose: bool = False) -> str:
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
         native = ex.submit(_native)
         objs = list(ex.map(_compile, SOURCES + BENCH_SOURCES))
-        native.result()
     _link(LIB, objs[:len(SOURCES)])
     # the benchmark library finds libmohge.so next to itself
     _link(BENCH_LIB, objs[len(SOURCES):], ["-L", HERE, "-lmohge", "-Wl,-rpath,$ORIGIN"])
+    module = native.result()                   # (raises only now: the libraries are there)
     if verbose:
-        print("built", LIB, BENCH_LIB, "and", NATIVE)
+        print("built", *filter(None, (LIB, BENCH_LIB, module)))
     return LIB
 
 
