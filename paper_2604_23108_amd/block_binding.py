@@ -45,7 +45,11 @@ def _call(name):
 class _Native:
     """The extension module, loaded and given the library's entry points at the first call."""
 
+    CALLS = ("rmsnorm", "rmsnorm_bwd", "cache_append", "cache_attention", "proj_w4")
+
     def __getattr__(self, name):
+        if name not in self.CALLS and name != "file":
+            raise AttributeError(f"_block_native has no {name}")
         from .build import native_path
         path = native_path(torch.__version__)
         if not os.path.exists(path):
@@ -53,10 +57,9 @@ class _Native:
         spec = importlib.util.spec_from_file_location("_block_native", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        entries = ("mohge_rmsnorm", "mohge_rmsnorm_bwd", "mohge_cache_append", "mohge_cache_attention", "mohge_proj_w4",
-                   "mohge_last_error")
+        entries = [f"mohge_{n}" for n in self.CALLS + ("last_error",)]
         module.bind(MohgeError, *[C.cast(getattr(lib(), e), C.c_void_p).value for e in entries])
-        for n in ("rmsnorm", "rmsnorm_bwd", "cache_append", "cache_attention", "proj_w4"):
+        for n in self.CALLS:
             setattr(self, n, getattr(module, n))
         self.file = path
         return self.__dict__[name]

@@ -49,3 +49,9 @@ def test_a_module_for_another_torch_is_not_loaded(monkeypatch):
     monkeypatch.setattr(torch, "__version__", "0.0.1")
     with pytest.raises(M.MohgeError, match="0.0.1.* is missing: build it"):
         B._Native().rmsnorm
+
+
+def test_names_that_the_module_lacks_are_attribute_errors():
+    with pytest.raises(AttributeError, match="no_such_call"):
+        B._native.no_such_call
+    assert not hasattr(B._native, "__wrapped__")
