@@ -133,6 +133,7 @@ typedef struct mohge_proj_config {
  *      low four bits; scales DEVICE [n_out, n_in/group] bf16; zeros DEVICE [n_out, n_in/group] bytes 0..15, or NULL: 8.
  * Out: y DEVICE [T, n_out].
  * Codes and x are exact in the matrix cores' bf16 operands; sums are fp32, a group's sum is multiplied by its scale.
+ * Infinite x give what the definition gives (infinities, NaN where a code is its zero point or both signs meet); such rows take longer.
  */
 int mohge_proj_w4(const mohge_proj_config* cfg, const void* x, const float* x_scale, const void* codes,
                   const void* scales, const void* zeros, void* y, void* stream);

@@ -233,8 +233,47 @@ __device__ __forceinline__ void multiply(const Batch<GROUP, RT, U, Z>& b, const 
   }
 }
 
-template <bool E4M3, int RT, int NT>
+// A sum straight from its definition
+template <int GROUP, bool Z, bool E4M3>
+__device__ __forceinline__ float direct_sum(const ProjArgs& a, const int r, const int n) {
+  const int groups = a.n_in / GROUP;
+  float sum = 0.f;
+#pragma unroll 1
+  for (int g = 0; g < groups; ++g) {
+    const long long at = (long long)n * groups + g;
+    const uint32_t* codes = reinterpret_cast<const uint32_t*>(a.codes) + at * (GROUP / 8);
+    float z = 8.f, part = 0.f;
+    if constexpr (Z) z = (float)a.zeros[at];
+#pragma unroll 1
+    for (int i = 0; i < GROUP / 8; ++i) {
+      const long long piece = ((long long)r * a.n_in + g * GROUP) / 8 + i;
+      float x[8];
+      if constexpr (E4M3) {
+        const uint2 d = static_cast<const uint2*>(a.x)[piece];
+        const auto u0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d.x, false), u1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d.x, true);
+        const auto v0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d.y, false), v1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)d.y, true);
+        x[0] = u0[0]; x[1] = u0[1]; x[2] = u1[0]; x[3] = u1[1]; x[4] = v0[0]; x[5] = v0[1]; x[6] = v1[0]; x[7] = v1[1];
+      } else {
+        Piece<true> p;
+        p.load(a.x, piece);
+        p.get(x);
+      }
+      const uint32_t c = codes[i];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) part = fmaf((float)((c >> (4 * j)) & 15u) - z, x[j], part);
+    }
+    sum = fmaf(__uint_as_float((uint32_t)a.scales[at] << 16), part, sum);
+    if (sum != sum) break;                        // NaN stays
+  }
+  return sum;
+}
+
+// Sums that are not finite are worked out again: the offset of 16 in front of the codes turns an infinite x into NaN, and overflows for
+// numbers that the definition's products still hold.  (Calls without such sums take as long
+// as without this; 32 rows, 65001 x 4096 45 us, with an infinite number in one row 0.3 ms.)
+template <int GROUP, bool Z, bool E4M3, int RT, int NT>
 __device__ __forceinline__ void store_rows(const ProjArgs& a, const int n0, const int m, const int q, const f32x4 (&acc)[RT][NT]) {
+  unsigned again = 0;
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -250,10 +289,20 @@ __device__ __forceinline__ void store_rows(const ProjArgs& a, const int n0, cons
             const long long at = (long long)r * a.n_out + n;
             if (a.f32) static_cast<float*>(a.y)[at] = acc[f][t][i] * xs;
             else static_cast<uint16_t*>(a.y)[at] = (uint16_t)pack_bf16x2(acc[f][t][i] * xs, 0.f);
+            if (!(fabsf(acc[f][t][i]) < INFINITY)) again |= 1u << ((t * 4 + i) * RT + f);
           }
         }
       }
     }
+  while (again) {
+    const int e = __builtin_ctz(again), r = 16 * (e / (4 * RT)) + 4 * q + e / RT % 4, n = n0 + 16 * (e % RT) + m;
+    again &= again - 1;
+    float sum = direct_sum<GROUP, Z, E4M3>(a, r, n);
+    if constexpr (E4M3) sum *= a.x_scale[r];
+    const long long at = (long long)r * a.n_out + n;
+    if (a.f32) static_cast<float*>(a.y)[at] = sum;
+    else static_cast<uint16_t*>(a.y)[at] = (uint16_t)pack_bf16x2(sum, 0.f);
+  }
 }
 
 // Few weight rows: a workgroup has 16 of them, its KW waves a part of the reduction each.  A wave stages its own part of x, U
@@ -337,7 +386,7 @@ __global__ void __launch_bounds__(64 * KW) proj_w4_split_kernel(const ProjArgs a
   for (int x = 0; x < KW - 1; ++x)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[0][t] += red[(x * NT + t) * 64 + lane];
-  store_rows<E4M3, 1, NT>(a, n0, m, q, acc);
+  store_rows<GROUP, Z, E4M3, 1, NT>(a, n0, m, q, acc);
 }
 
 // Many weight rows: every wave has 16 RT of its own and the whole reduction; the workgroup's waves share the staged rows of x, U units
@@ -407,7 +456,7 @@ __global__ void __launch_bounds__(256, 2) proj_w4_kernel(const ProjArgs a) {
     turn();
   }
   compute(from);
-  store_rows<E4M3, RT, NT>(a, n0, m, q, acc);
+  store_rows<GROUP, Z, E4M3, RT, NT>(a, n0, m, q, acc);
 }
 
 template <int GROUP, int NT, int RT, int P, bool Z, bool E4M3>
