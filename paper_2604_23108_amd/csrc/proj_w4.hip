@@ -10,6 +10,8 @@
 //                       (E4M3 rows of x become bf16 as well.  As E4M3 numbers, which the codes' bytes are by themselves in units of
 //                       2^-9, the products need half the instructions, but v_mfma_f32_16x16x32_fp8_fp8 drops bits when it adds
 //                       them: results 5e-5 off, where this form's are 2e-7.)
+//                       (It makes a group's sums several times the result, at no bias: for x and weights of one sign, the worst case, with
+//                       groups of 128 the errors are at most 6e-7 of the sum of |w x|, their mean below 2e-8 of it.)
 //   sums of x           a product with ones gives sum_{k in g} x_tk in the lanes that need it.
 //   groups              one product reduces 8 codes of each of four lanes; with groups of 128 those are in one group as
 //                       loaded, for 64 and 32 the lanes exchange words first (v_permlane32_swap, v_permlane16_swap).
