@@ -290,12 +290,12 @@ struct Stretches {
   __device__ __forceinline__ int last_of(int r0, int units) const { return udiv(r0 + units - 1, per); }
 };
 
-// What a part adds to its row's counter.  Odd and far from every small number's multiple, another one for another number of parts: only a
-// counter that was 0 comes to parts * part_unit(parts), at the last part.  From any other start (numbers that the memory held, what calls
-// that overlapped left) it does not, in this call or a later one; counted by ones, a counter of 1 would have parts joined that are not
-// written yet, and be 1 again afterwards.  (2^64 over the golden ratio, and 2^64 (sqrt 2 - 1).)
+// What a part adds to its row's counter: an odd number, whose first 2^24 multiples all lie 2^34 and more away from 0 (mod 2^64), another one for
+// another number of parts.  So only a counter that was 0 comes to parts * part_unit(parts), at the last part; from another start (small
+// numbers that the memory held, what calls that overlapped left) it does not, in this call or a later one.  Counted by ones, a counter of
+// 1 would have parts joined that are not written yet, and be 1 again afterwards.  (2^64 over the golden ratio, and 2^64 (sqrt 2 - 1).)
 __device__ __forceinline__ unsigned long long part_unit(int parts) {
-  return 0x9e3779b97f4a7c15ull + (unsigned long long)parts * 0x6a09e667f3bcc909ull;
+  return 0x9e3779b97f4a7c15ull + (unsigned long long)parts * 0x6a09e667f3bcc908ull;
 }
 
 // A row of which this workgroup has a part
