@@ -37,7 +37,8 @@ typedef struct mohge_norm_config {
  * In:  x DEVICE [T,d]; residual DEVICE [T,d] or NULL; weight DEVICE [d] f32.
  * Out: sum_out DEVICE [T,d] = h or NULL (may be x or residual itself); y DEVICE [T,d]; y_scale DEVICE [T] f32,
  *      required for MOHGE_E4M3 and NULL otherwise; rstd DEVICE [T] f32 or NULL (the backward pass reads it).
- * The statistic and y are those of the fp32 sum, before it is rounded for sum_out.
+ * The statistic and y are those of the fp32 sum, before it is rounded for sum_out.  (A row whose sum of squares passes the largest fp32
+ * number has rstd = 0 and y = 0.)
  */
 int mohge_rmsnorm(const mohge_norm_config* cfg, const void* x, const void* residual, const float* weight,
                   void* sum_out, void* y, float* y_scale, float* rstd, void* stream);
@@ -96,7 +97,8 @@ int mohge_cache_append(const mohge_cache_config* cfg, int32_t n_tokens, const vo
 /*
  * Attention of one query row per sequence over all its positions, n = seq_lens[b]:
  *   s_j = scale q . k_j,   out = sum_{j<n} softmax(s)_j v_j,   lse = log sum_{j<n} exp s_j.
- * A sequence of length 0 gives out = 0 and lse = -infinity.
+ * A sequence of length 0, or whose scores are all -infinity, gives out = 0 and lse = -infinity.  An infinite value in a position that counts
+ * gives an infinite element or NaN.
  * In:  q DEVICE [n_seqs, n_heads, head_size] (dtype), q_stride elements from sequence to sequence (a multiple of 8, at
  *      least n_heads * head_size).
  * Out: out DEVICE [n_seqs, n_heads, head_size] (dtype); lse DEVICE [n_seqs, n_heads] f32 or NULL.

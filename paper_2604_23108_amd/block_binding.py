@@ -171,7 +171,7 @@ class ResidualNorm:
             self.ws = torch.empty(max(16, mohge_norm_workspace_size(cfg)), dtype=torch.uint8, **dev)
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """y; the new residual stream is left in `sum` (without a residual it is x itself)."""
+        """y; the new residual stream is left in `sum` (without a residual it is x itself, which `backward` then reads again)."""
         out = None if residual is None else self.sum
         mohge_rmsnorm(self.cfg, x, residual, self.weight, out, self.y, self.y_scale, self.rstd)
         self._h = x if residual is None else self.sum

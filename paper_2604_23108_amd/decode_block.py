@@ -3,7 +3,7 @@ attention over it, norm, MoHGE layer.
 
     python -m paper_2604_23108_amd.decode_block --seqs 32 --steps 20
 
-runs such a block with random weights and prints the time of a step.  Position embeddings and sampling are the
+runs such a block with random weights, over a cache filled with random rows, and prints the time of a step.  Position embeddings and sampling are the
 caller's; several blocks are stacked by handing `forward`'s two results to the next one.
 """
 from __future__ import annotations
