@@ -8,8 +8,8 @@
  * mohge.h: calls only enqueue kernels, allocate nothing and keep nothing.  Sums, statistics and softmax
  * weights are fp32.  E4M3 codes (one byte each) and their conversion are those of mohge_expert_ffn_w8:
  * the value is scale * value(code), where a row of n values x has
- *   scale = max(max|x| / 448, 2^-126), or 1 for a row of zeros, and code = x / scale rounded to nearest even
- * (both quotients are fp32, rounded to nearest).
+ *   scale = max(max|x| * (1/448), 2^-126), or 1 for a row of zeros, and code = x * (1/scale) rounded to nearest even,
+ * reciprocals and products in fp32, each rounded to nearest.  (For bf16 x the codes are those of x / scale too.)
  */
 #ifndef MOHGE_BLOCK_H
 #define MOHGE_BLOCK_H

@@ -78,9 +78,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_kernel(
   }
   if (row >= T) return;
   const float rstd = rsqrtf(ss * inv_d + eps);
-  float scale = 1.f;
+  float scale = 1.f, inv_scale = 1.f;
   if constexpr (Q8) {
     scale = e4m3_scale(top * rstd);          // top * rstd is the largest |y| as it is rounded below: rounding keeps the order
+    inv_scale = 1.f / scale;
     if (t == 0) y_scale[row] = scale;
   }
   if (rstd_out && t == 0) rstd_out[row] = rstd;
@@ -96,8 +97,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_kernel(
       float v[8];
       if constexpr (Q8) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = h[i][j] * w[i][j] * rstd;
-        divide_by_scale<2>(v, scale);
+        for (int j = 0; j < 8; ++j) v[j] = h[i][j] * w[i][j] * rstd * inv_scale;
         static_cast<uint2*>(y)[base + p] = to_e4m3x8(v);
       } else {
 #pragma unroll

