@@ -13,7 +13,8 @@
 //             lane (m, q) loads rows 4q..4q+3 of V, elements m D/16 .. (m+1) D/16 - 1, in one access per row, and turns
 //             two rows into pairs by v_perm.  Result j of the lane is element (D/16) (4q + i) + j of head m's output.
 // The weights are split into two bf16 parts (the rest after the first is below 2^-17 of it), which costs one more
-// product and keeps them as good as fp32: one bf16 rounding of them would be as large as the output's own.
+// product: one bf16 rounding of them would be as large as the output's own.  (32 ragged sequences up to 8191: 280 of 131072 bf16 outputs are not
+// the rounded exact value, 62 to 94 where everything is fp32.)
 // fp32 caches go through the fp32 matrix cores (16x16x4) with the same assignment, four positions at a time.
 //
 // Work split: the positions of every (sequence, kv head, block of 16 query heads) are cut into units of four tiles, one for each wave (128
